@@ -205,6 +205,36 @@ int ab_dense_backward(const void* x, const void* dY, const void* W, void* dX, fl
                       int64_t N, int m, int n, int dt, void* ws, size_t ws_bytes, void* cuda_stream);
 
 /*
+ * Low-rank adapters of many requests, or of many training groups, beside one shared projection.  (The paper's workers each train
+ * factors of their own, Algorithm 1; here the factors of L workers, or of L fine-tunings of one dense weight, lie side by side in one
+ * device's memory and every row of a batch goes through its own pair.)
+ *   row_adapter: int32 [N] on the device; with a = row_adapter[i]:
+ *   forward : T_i = s_a B_a x_i,  y_i = W x_i + A_a T_i                      (s_a = scale[a], 1 where scale is NULL)
+ *   backward: U_i = s_a A_a^T dY_i,  dX_i = W^T dY_i + B_a^T U_i,
+ *             dA_a = sum of dY_i T_i^T,  dB_a = sum of U_i x_i^T over the rows i of adapter a.
+ *   An entry of -1 stands for a row without an adapter (also a padded one): y_i = W x_i, dX_i = W^T dY_i, no part in dA, dB.  Rows of an
+ *   adapter may lie anywhere; runs of rows are faster.  Any other entry outside 0 .. L-1 counts as -1 and the first int of ws receives
+ *   AB_ERR_INVALID_ARG (else AB_OK, or AB_ERR_TIMEOUT as for ab_layer_forward).
+ *   x [N,n], W [m,n], y, dY [N,m], dX [N,n] dense, of type dt; A: L matrices [m,r], matrix a at A + a*strideA elements; B: L matrices
+ *   [r,n], matrix a at B + a*strideB; scale: fp32 [L] or NULL.  1 <= r <= min(m,n).  strideA, strideB are ignored for L = 1.
+ *   T_save: NULL, or fp32 [N,r] that receives T (0 in rows without an adapter) for the backward call; T_saved NULL recomputes it from x.
+ *   dA [L,m,r], dB [L,r,n]: fp32, dense, every element written: 0 for an adapter without rows.  W is not trained here (ab_dense_backward
+ *   has dW).  Any of dX, dA, dB may be NULL; W may be NULL where dX is.
+ *   Sums are held in fp32 or more and y, dX rounded once.  Sums run in a fixed order: two runs give identical bits.  No row's result
+ *   depends on another row, nor on an adapter that is not its own, also where those hold infinities or NaN; nor does dA_a or dB_a on rows
+ *   that are not a's.  bf16 with m, n, r, strideA, strideB multiples of 8, r <= 256 and 16-byte aligned pointers runs on the tensor cores;
+ *   everything else takes general kernels.  N = 0 is a no-op (dA, dB are zeroed).  N < 2^31.  No output may overlap an input or
+ *   another output.  Workspace: ab_adapter_workspace_bytes, for either call.
+ */
+int ab_adapter_forward(const void* x, const void* W, const void* A, const void* B, const float* scale, const int* row_adapter,
+                       void* y, float* T_save, int64_t N, int m, int n, int r, int L, int64_t strideA, int64_t strideB, int dt,
+                       void* ws, size_t ws_bytes, void* cuda_stream);
+int ab_adapter_backward(const void* x, const void* dY, const void* W, const void* A, const void* B, const float* scale,
+                        const int* row_adapter, const float* T_saved, void* dX, float* dA, float* dB, int64_t N, int m, int n, int r,
+                        int L, int64_t strideA, int64_t strideB, int dt, void* ws, size_t ws_bytes, void* cuda_stream);
+size_t ab_adapter_workspace_bytes(int64_t N, int m, int n, int r, int L, int dt);
+
+/*
  * One AdamW update of a factor from the gradient ab_layer_backward left (the paper trains with
  * AdamW, Section "Experiments"; decoupled weight decay):
  *   p <- p (1 - lr wd);  m <- b1 m + (1-b1) g;  v <- b2 v + (1-b2) g^2;

@@ -12,6 +12,9 @@ What each function follows:
   trailing dimensions (Methodology, after Eq. 3) applied to NHWC activations.
 * ``dense_forward`` / ``dense_backward``  the same layer with W dense (Algorithm 1's
   full-rank steps: warm-up and rebound).
+* ``adapter_forward`` / ``adapter_backward``  the factorised layer beside a dense weight, every row
+  with a pair of its own (Algorithm 1's workers side by side on one device).
+* ``grad_clip``                norm over all gradients of a step, and their scaling.
 * ``group_average*``           Algorithm 1, the two allReduce(./worldSize) lines.
 * ``recombine``                Algorithm 1, "W <- AB".
 * ``jacobi_svd``               the SVD that Eq. 3 refers to (one-sided Jacobi,
@@ -275,6 +278,43 @@ def lr_rebound_factor(steps_since_change, rebound_steps, floor=0.0):
     if rebound_steps <= 0 or steps_since_change >= rebound_steps:
         return 1.0
     return floor + (1.0 - floor) * max(0, steps_since_change) / rebound_steps
+
+
+def adapter_forward(x, W, A, B, row_adapter, scale=None):
+    """Factor pairs of many requests beside one dense weight: (T, y) with T_i = s_a B_a x_i, y_i = W x_i + A_a T_i, a =
+    row_adapter[i]; rows whose entry is no index of A have T_i = 0 and y_i = W x_i."""
+    x, W, A, B = _f64(x), _f64(W), _f64(A), _f64(B)
+    T = np.zeros((x.shape[0], A.shape[2]))
+    y = x @ W.T
+    for a in range(A.shape[0]):
+        rows = np.flatnonzero(np.asarray(row_adapter) == a)
+        if rows.size:
+            T[rows] = (1.0 if scale is None else float(scale[a])) * (x[rows] @ B[a].T)
+            y[rows] += T[rows] @ A[a].T
+    return T, y
+
+
+def adapter_backward(x, dY, W, A, B, row_adapter, scale=None):
+    """Gradients of adapter_forward: (dX, dA, dB)."""
+    x, dY, W, A, B = _f64(x), _f64(dY), _f64(W), _f64(A), _f64(B)
+    dX, dA, dB = dY @ W, np.zeros(A.shape), np.zeros(B.shape)
+    for a in range(A.shape[0]):
+        rows = np.flatnonzero(np.asarray(row_adapter) == a)
+        if rows.size:
+            s = 1.0 if scale is None else float(scale[a])
+            U = s * (dY[rows] @ A[a])
+            dX[rows] += U @ B[a]
+            dA[a] = dY[rows].T @ (s * (x[rows] @ B[a].T))
+            dB[a] = U.T @ x[rows]
+    return dX, dA, dB
+
+
+def grad_clip(grads, max_norm):
+    """(scaled gradients, norm): the norm over all of them; above max_norm all are scaled by max_norm / norm.  A norm that is no
+    finite number scales nothing."""
+    norm = float(np.sqrt(sum(float((_f64(g) ** 2).sum()) for g in grads)))
+    c = max_norm / norm if np.isfinite(norm) and norm > max_norm else 1.0
+    return [c * _f64(g) for g in grads], norm
 
 
 def rel_frob(a, b):

@@ -28,7 +28,8 @@ EXPORTS = ["ab_status_string", "ab_version", "ab_launch_count", "ab_workspace_by
            "ab_selftest_chain_stall", "ab_selftest_chain_stall_workspace_bytes",
            "ab_selftest_split_fallback", "ab_selftest_split_fallback_workspace_bytes",
            "ab_dense_forward", "ab_dense_backward", "ab_conv3x3_forward", "ab_conv3x3_backward",
-           "ab_conv3x3_workspace_bytes", "ab_recombine_mean"]
+           "ab_conv3x3_workspace_bytes", "ab_recombine_mean", "ab_adapter_forward", "ab_adapter_backward",
+           "ab_adapter_workspace_bytes"]
 
 
 class AbError(RuntimeError):
@@ -65,6 +66,12 @@ def lib() -> ctypes.CDLL:
     L.ab_layer_forward.argtypes = [c_void_p] * 5 + [c_int64] + [c_int] * 6 + [c_void_p, c_size_t, c_void_p]
     L.ab_layer_backward.restype = c_int
     L.ab_layer_backward.argtypes = [c_void_p] * 8 + [c_int64] + [c_int] * 6 + [c_void_p, c_size_t, c_void_p]
+    L.ab_adapter_forward.restype = c_int
+    L.ab_adapter_forward.argtypes = [c_void_p] * 8 + [c_int64] + [c_int] * 4 + [c_int64] * 2 + [c_int, c_void_p, c_size_t, c_void_p]
+    L.ab_adapter_backward.restype = c_int
+    L.ab_adapter_backward.argtypes = [c_void_p] * 11 + [c_int64] + [c_int] * 4 + [c_int64] * 2 + [c_int, c_void_p, c_size_t, c_void_p]
+    L.ab_adapter_workspace_bytes.restype = c_size_t
+    L.ab_adapter_workspace_bytes.argtypes = [c_int64] + [c_int] * 5
     L.ab_group_average.restype = c_int
     L.ab_group_average.argtypes = [c_void_p, c_int64, c_int, c_int64, c_int, c_int, c_void_p, c_void_p]
     L.ab_recombine.restype = c_int
@@ -318,6 +325,79 @@ def ab_dense_backward(x, dY, W, want=("dX", "dW"), dX=None, dW=None, ws=None, st
                                  _stream(stream))
     _check(st, "ab_dense_backward")
     return dX, dW
+
+
+def ab_adapter_workspace_bytes(x, A, B) -> int:
+    """Scratch bytes of ab_adapter_forward and ab_adapter_backward for rows x (N, n) and adapters A (L, m, r), B (L, r, n)."""
+    L, m, r = A.shape
+    return int(lib().ab_adapter_workspace_bytes(x.shape[0], m, B.shape[2], r, L, _dt(x)))
+
+
+def _adapter_ok(x, W, A, B, row_adapter, scale, dY, outs, f32):
+    """Shapes, types and places of the tensors of an adapter call.  A and B may be spaced along their first axis."""
+    if x.dim() != 2 or A.dim() != 3 or B.dim() != 3:
+        raise ValueError("x is (N, n), A (L, m, r), B (L, r, n)")
+    N, n = x.shape
+    L, m, r = A.shape
+    if B.shape != (L, r, n) or (W is not None and W.shape != (m, n)):
+        raise ValueError(f"A {tuple(A.shape)}, B {tuple(B.shape)} and W do not fit rows of {n}")
+    if row_adapter.shape != (N,) or row_adapter.dtype != torch.int32 or (scale is not None and (scale.shape != (L,) or scale.dtype != torch.float32)):
+        raise ValueError("row_adapter is int32 (N,), scale fp32 (L,)")
+    _dev_ok(x, W, row_adapter, scale, dY, *(t for t, _ in outs), *(t for t, _ in f32))
+    for t in (A, B):
+        if not t.is_cuda or (L > 0 and not t[0].is_contiguous()):
+            raise ValueError("each adapter's matrix must be a contiguous CUDA tensor")
+    for t in (W, A, B, dY) + tuple(t for t, _ in outs):
+        if t is not None and t.dtype != x.dtype:
+            raise ValueError("x, W, A, B, dY and their results have one type")
+    for t, shape in outs + f32 + (((dY, (N, m)),) if dY is not None else ()):
+        if t is not None and tuple(t.shape) != shape:
+            raise ValueError(f"expected a tensor of {shape}, got {tuple(t.shape)}")
+    dev = torch.cuda.current_device()
+    for t in (x, W, A, B, row_adapter, scale, dY) + tuple(t for t, _ in outs) + tuple(t for t, _ in f32):
+        if t is not None and t.device.index != dev:
+            raise ValueError("tensors must be on the current device")
+    for t, _ in f32:
+        if t is not None and t.dtype != torch.float32:
+            raise ValueError("T, dA and dB are fp32")
+
+
+def ab_adapter_forward(x, W, A, B, row_adapter, scale=None, y=None, T_save=None, ws=None, stream=None, save_T=False):
+    """y_i = W x_i + scale_a A_a (B_a x_i) with a = row_adapter[i] (-1: W x_i alone).  x (N, n), W (m, n), A (L, m, r),
+    B (L, r, n), row_adapter int32 (N,), scale fp32 (L,) or None.  Returns (y, T (N, r) fp32 or None)."""
+    N, L, m, r = x.shape[0], *A.shape
+    _adapter_ok(x, W, A, B, row_adapter, scale, None, ((y, (N, m)),), ((T_save, (N, r)),))
+    if y is None:
+        y = torch.empty((N, m), dtype=x.dtype, device=x.device)
+    if save_T and T_save is None:
+        T_save = torch.empty((N, r), dtype=torch.float32, device=x.device)
+    if ws is None:
+        ws = workspace(ab_adapter_workspace_bytes(x, A, B), x.device)
+    st = lib().ab_adapter_forward(_ptr(x), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(row_adapter), _ptr(y), _ptr(T_save), N, m,
+                                  x.shape[1], r, L, A.stride(0), B.stride(0), _dt(x), _ptr(ws), ws.numel(), _stream(stream))
+    _check(st, "ab_adapter_forward")
+    return y, T_save
+
+
+def ab_adapter_backward(x, dY, W, A, B, row_adapter, scale=None, T_saved=None, want=("dX", "dA", "dB"), dX=None, dA=None, dB=None,
+                        ws=None, stream=None):
+    """Gradients of ab_adapter_forward: dX (N, n), dA (L, m, r) and dB (L, r, n) in fp32; entries not in `want` are None.  T_saved is
+    the T of the forward call, or None to recompute it.  W may be None where dX is not wanted."""
+    N, n, L, m, r = *x.shape, *A.shape
+    _adapter_ok(x, W, A, B, row_adapter, scale, dY, ((dX, (N, n)),), ((T_saved, (N, r)), (dA, (L, m, r)), (dB, (L, r, n))))
+    if "dX" in want and dX is None:
+        dX = torch.empty((N, n), dtype=x.dtype, device=x.device)
+    if "dA" in want and dA is None:
+        dA = torch.empty((L, m, r), dtype=torch.float32, device=x.device)
+    if "dB" in want and dB is None:
+        dB = torch.empty((L, r, n), dtype=torch.float32, device=x.device)
+    if ws is None:
+        ws = workspace(ab_adapter_workspace_bytes(x, A, B), x.device)
+    st = lib().ab_adapter_backward(_ptr(x), _ptr(dY), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(row_adapter), _ptr(T_saved), _ptr(dX),
+                                   _ptr(dA), _ptr(dB), N, m, n, r, L, A.stride(0), B.stride(0), _dt(x), _ptr(ws), ws.numel(),
+                                   _stream(stream))
+    _check(st, "ab_adapter_backward")
+    return dX, dA, dB
 
 
 def ab_adamw_step(param, grad, m, v, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=1e-2, param_bf16=None,

@@ -1,0 +1,63 @@
+"""Host-side refusals of the adapter calls: bad arguments are answered before anything is launched.  No GPU needed."""
+import ctypes
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2405_01067_b200 import build
+    build.build()
+    from paper_2405_01067_b200 import binding
+    binding.lib()
+    return binding
+
+
+P = ctypes.c_void_p(4096)          # never dereferenced: every call below fails its checks first
+
+
+def forward(b, **kw):
+    a = dict(x=P, W=P, A=P, B=P, scale=None, ids=P, y=P, T=None, N=4, m=16, n=24, r=8, L=2, sA=128, sB=192, dt=b.AB_BF16, ws=P,
+             ws_bytes=1 << 30) | kw
+    return b.lib().ab_adapter_forward(*a.values(), None)
+
+
+def backward(b, **kw):
+    a = dict(x=P, dY=P, W=P, A=P, B=P, scale=None, ids=P, T=None, dX=P, dA=P, dB=P, N=4, m=16, n=24, r=8, L=2, sA=128, sB=192,
+             dt=b.AB_BF16, ws=P, ws_bytes=1 << 30) | kw
+    return b.lib().ab_adapter_backward(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw", [dict(x=None), dict(A=None), dict(B=None), dict(ids=None), dict(N=-1), dict(m=0), dict(n=0), dict(r=0), dict(r=17),
+                                dict(L=0), dict(L=-3), dict(sA=127), dict(sB=191), dict(dt=2), dict(x=ctypes.c_void_p(4097)),
+                                dict(A=ctypes.c_void_p(4097)), dict(ids=ctypes.c_void_p(4098))])
+def test_bad_arguments_of_both(b, kw):
+    assert forward(b, **kw) == b.AB_ERR_INVALID_ARG
+    assert backward(b, **kw) == b.AB_ERR_INVALID_ARG
+
+
+def test_bad_arguments_of_one(b):
+    assert forward(b, W=None) == b.AB_ERR_INVALID_ARG
+    assert forward(b, y=None) == b.AB_ERR_INVALID_ARG
+    assert forward(b, T=ctypes.c_void_p(4098)) == b.AB_ERR_INVALID_ARG
+    assert backward(b, dY=None) == b.AB_ERR_INVALID_ARG
+    assert backward(b, W=None) == b.AB_ERR_INVALID_ARG
+    assert backward(b, dA=ctypes.c_void_p(4098)) == b.AB_ERR_INVALID_ARG
+    assert forward(b, N=1 << 31) == b.AB_ERR_UNSUPPORTED
+    assert backward(b, N=1 << 31) == b.AB_ERR_UNSUPPORTED
+
+
+def test_workspace_query(b):
+    q = b.lib().ab_adapter_workspace_bytes
+    assert q(64, 256, 512, 32, 2, b.AB_F32) >= 256
+    assert q(0, 256, 512, 32, 2, b.AB_BF16) >= 256
+    for bad in ((-1, 256, 512, 32, 2, 0), (64, 0, 512, 32, 2, 0), (64, 256, 512, 0, 2, 0), (64, 256, 512, 32, 0, 0), (64, 256, 512, 32, 2, 7),
+                (1 << 31, 256, 512, 32, 2, 0)):
+        assert q(*bad) == 0
+
+
+def test_no_device_means_an_error(b):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    assert forward(b) == b.AB_ERR_CUDA and backward(b) == b.AB_ERR_CUDA
