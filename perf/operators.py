@@ -139,11 +139,11 @@ def prepare(case, seed):
 def _run_own(s):
     from paper_2405_01067_b200 import binding as ab
     if s["op"] == "clip":
-        if "ws" not in s:                        # a program keeps its workspace
-            s["ws"] = ab.workspace(ab.ab_grad_clip_workspace_bytes(s["grads"]), "cuda")
-        _, norm = ab.ab_grad_clip(s["grads"], s["max_norm"], out=s["outs"], ws=s["ws"])
+        if "plan" not in s:                      # a program whose gradients stay where they are keeps their list
+            s["plan"] = ab.ClipPlan(s["grads"], out=s["outs"])
+        _, norm = ab.ab_grad_clip(s["plan"], s["max_norm"])
         return {"out": s["whole"], "norm": norm}
-    if "ws" not in s:
+    if "ws" not in s:                            # and its workspace
         s["ws"] = ab.workspace(ab.ab_adapter_workspace_bytes(s["x"], s["A"], s["B"]), "cuda")
     if s["op"] == "forward":
         y, _ = ab.ab_adapter_forward(s["x"], s["W"], s["A"], s["B"], s["map"], scale=s["scale"], ws=s["ws"])
