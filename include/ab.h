@@ -248,6 +248,25 @@ int ab_adamw_step(float* param, const float* grad, float* m, float* v, void* par
                   float lr, float beta1, float beta2, float eps, float weight_decay, int step,
                   void* cuda_stream);
 
+/* One tensor of a gradient clipping.  Device pointers; out may be grad itself. */
+typedef struct {
+  const void* grad;       /* [count] */
+  void* out;              /* [count], or NULL in every descriptor: only the norm is wanted */
+  int64_t count;
+} ab_clip_desc;
+
+/*
+ * Global norm of the gradients of a step and their scaling, between the backward calls and ab_adamw_step:
+ *   norm = sqrt(sum of g^2 over all L tensors);  out = g * c,  c = max_norm / norm where norm > max_norm, else 1.
+ * descs: HOST array of L descriptors (read before the call returns); tensors of type dt that start at any element; outputs overlap nothing
+ * but their own gradient, if at all.  norm_out: device float.  Squares are added in 64 bits in a fixed order (no finite value
+ * overflows; two runs give identical bits); out is rounded once from fp32.  A norm that is infinite or NaN scales nothing (out = g), so
+ * that the caller, who finds it in norm_out, can drop the step.  max_norm >= 0; INFINITY never scales.  In place and with c = 1 nothing
+ * is written.  Workspace: ab_grad_clip_workspace_bytes.
+ */
+int ab_grad_clip(const ab_clip_desc* descs, int L, float max_norm, float* norm_out, int dt, void* ws, size_t ws_bytes, void* cuda_stream);
+size_t ab_grad_clip_workspace_bytes(int L);
+
 /*
  * Learning-rate rebound (Section "Methodology", "learning rate rebound"): whenever the parameters
  * change shape the rate drops to near zero and climbs back to its scheduled value over

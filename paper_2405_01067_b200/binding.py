@@ -29,7 +29,7 @@ EXPORTS = ["ab_status_string", "ab_version", "ab_launch_count", "ab_workspace_by
            "ab_selftest_split_fallback", "ab_selftest_split_fallback_workspace_bytes",
            "ab_dense_forward", "ab_dense_backward", "ab_conv3x3_forward", "ab_conv3x3_backward",
            "ab_conv3x3_workspace_bytes", "ab_recombine_mean", "ab_adapter_forward", "ab_adapter_backward",
-           "ab_adapter_workspace_bytes"]
+           "ab_adapter_workspace_bytes", "ab_grad_clip", "ab_grad_clip_workspace_bytes"]
 
 
 class AbError(RuntimeError):
@@ -42,6 +42,10 @@ class ab_sync_desc(ctypes.Structure):
     _fields_ = [("A_copies", c_void_p), ("B_copies", c_void_p), ("strideA", c_int64), ("strideB", c_int64),
                 ("m", c_int), ("n", c_int), ("r", c_int), ("A_out", c_void_p), ("B_out", c_void_p),
                 ("sigma", c_void_p), ("r_out", c_void_p), ("W_out", c_void_p)]
+
+
+class ab_clip_desc(ctypes.Structure):
+    _fields_ = [("grad", c_void_p), ("out", c_void_p), ("count", c_int64)]
 
 
 _lib = None
@@ -89,6 +93,10 @@ def lib() -> ctypes.CDLL:
     L.ab_static_scratch_elems.restype = c_size_t
     L.ab_adamw_step.restype = c_int
     L.ab_adamw_step.argtypes = [c_void_p] * 5 + [c_int64] + [c_float] * 5 + [c_int, c_void_p]
+    L.ab_grad_clip.restype = c_int
+    L.ab_grad_clip.argtypes = [ctypes.POINTER(ab_clip_desc), c_int, c_float, c_void_p, c_int, c_void_p, c_size_t, c_void_p]
+    L.ab_grad_clip_workspace_bytes.restype = c_size_t
+    L.ab_grad_clip_workspace_bytes.argtypes = [c_int]
     L.ab_lr_rebound_factor.restype = c_float
     L.ab_lr_rebound_factor.argtypes = [c_int, c_int, c_float]
     L.ab_selftest_bounded_wait.restype = c_int
@@ -413,6 +421,40 @@ def ab_adamw_step(param, grad, m, v, lr, step, beta1=0.9, beta2=0.999, eps=1e-8,
                              eps, weight_decay, step, _stream(stream))
     _check(st, "ab_adamw_step")
     return param
+
+
+class ClipPlan:
+    """Descriptors and workspace of the clipping of one step's gradients (ab_grad_clip): tensors of one type at addresses that stay, as
+    an optimizer's do.  out: tensors that receive the scaled values (None: in place); norm_only leaves the gradients alone."""
+
+    def __init__(self, grads, out=None, norm_only=False):
+        self.grads = list(grads)
+        self.out = None if norm_only else self.grads if out is None else list(out)
+        if not self.grads:
+            raise ValueError("no gradients")
+        outs = self.out if self.out is not None else [None] * len(self.grads)
+        if len(outs) != len(self.grads):
+            raise ValueError("as many outputs as gradients")
+        dev = torch.cuda.current_device()
+        self.dt = _dt(self.grads[0])
+        for g, o in zip(self.grads, outs):
+            _dev_ok(g, o)
+            if g.dtype != self.grads[0].dtype or (o is not None and (o.dtype != g.dtype or o.numel() != g.numel())):
+                raise ValueError("gradients and outputs have one type, and each output its gradient's size")
+            if g.device.index != dev or (o is not None and o.device.index != dev):
+                raise ValueError("tensors must be on the current device")
+        self.descs = (ab_clip_desc * len(self.grads))(*[(g.data_ptr(), None if o is None else o.data_ptr(), g.numel())
+                                                        for g, o in zip(self.grads, outs)])
+        self.norm = torch.zeros((), dtype=torch.float32, device=self.grads[0].device)
+        self.ws = workspace(lib().ab_grad_clip_workspace_bytes(len(self.grads)), self.grads[0].device)
+
+
+def ab_grad_clip(plan: ClipPlan, max_norm: float, stream=None):
+    """Scales the plan's gradients by max_norm / norm where their global norm is above max_norm.  Returns (outputs or None, norm), norm a
+    device tensor of one fp32 value; one that is not finite scales nothing."""
+    st = lib().ab_grad_clip(plan.descs, len(plan.grads), float(max_norm), _ptr(plan.norm), plan.dt, _ptr(plan.ws), plan.ws.numel(), _stream(stream))
+    _check(st, "ab_grad_clip")
+    return plan.out, plan.norm
 
 
 def ab_lr_rebound_factor(steps_since_change: int, rebound_steps: int, floor: float = 0.0) -> float:

@@ -61,3 +61,21 @@ def test_no_device_means_an_error(b):
     if torch.cuda.is_available():
         pytest.skip("a device is present")
     assert forward(b) == b.AB_ERR_CUDA and backward(b) == b.AB_ERR_CUDA
+
+
+def clip(b, tensors, **kw):
+    arr = (b.ab_clip_desc * max(1, len(tensors)))(*tensors)
+    a = dict(descs=arr, L=len(tensors), max_norm=1.0, norm=P, dt=b.AB_F32, ws=P, ws_bytes=1 << 20) | kw
+    return b.lib().ab_grad_clip(*a.values(), None)
+
+
+def test_clip_refusals(b):
+    good = [(4096, 8192, 10), (4100, 8196, 0)]
+    bad = b.AB_ERR_INVALID_ARG
+    assert clip(b, []) == bad and clip(b, good, descs=None) == bad and clip(b, good, norm=None) == bad and clip(b, good, dt=3) == bad
+    assert clip(b, good, max_norm=-1.0) == bad and clip(b, good, max_norm=float("nan")) == bad
+    assert clip(b, [(None, 4096, 3)]) == bad and clip(b, [(4096, 4096, -1)]) == bad and clip(b, [(4097, 8192, 3)]) == bad
+    assert clip(b, [(4096, 8194, 3)]) == bad
+    assert clip(b, [(4096, 4096, 3), (8192, None, 3)]) == bad          # all are scaled or none is
+    assert clip(b, [(4096, 4096, (1 << 40) + 1)]) == b.AB_ERR_UNSUPPORTED
+    assert b.lib().ab_grad_clip_workspace_bytes(0) == 0 and b.lib().ab_grad_clip_workspace_bytes(5) >= 256
