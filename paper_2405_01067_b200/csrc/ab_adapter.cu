@@ -9,7 +9,7 @@
 // over one row, or over the rows of one adapter, and nothing is masked by a multiplication with zero.
 #include <string.h>
 
-#include "ab_common.cuh"
+#include "ab_adapter.cuh"
 
 namespace ab {
 namespace {
@@ -217,16 +217,7 @@ adapter_grad_kernel(const TI* __restrict__ In, int P, const float* __restrict__ 
     if (k0 + 8 * kq + e < r) d[(k0 + 8 * kq + e) * d_k] = (float)acc[e];
 }
 
-struct Call {
-  const void *x, *W, *A, *B;
-  const float* scale;
-  const int* ids;
-  int64_t N;
-  int m, n, r, L;
-  int64_t strideA, strideB;
-  int dt;
-  cudaStream_t st;
-};
+typedef AdapterCall Call;
 
 // Workspace of the general path: status word, T, U, base of a bf16 result in fp32, the adapters' rows
 struct GeneralWs { int* status; float *T, *U, *base; int* order; int64_t *start, *count; size_t bytes; };
@@ -329,7 +320,9 @@ extern "C" {
 
 size_t ab_adapter_workspace_bytes(int64_t N, int m, int n, int r, int L, int dt) {
   if (N < 0 || N > 0x7fffffffll || m <= 0 || n <= 0 || r <= 0 || L <= 0 || !dtype_ok(dt)) return 0;
-  return general_ws(nullptr, N, m, n, r, L, dt).bytes + 256;
+  const size_t g = general_ws(nullptr, N, m, n, r, L, dt).bytes;
+  const size_t t = adapter_tc_shape_ok(N, m, n, r, L, dt) ? adapter_tc_ws(N, m, n, r, L) : 0;
+  return (g > t ? g : t) + 256;
 }
 
 int ab_adapter_forward(const void* x, const void* W, const void* A, const void* B, const float* scale, const int* row_adapter,
@@ -341,6 +334,10 @@ int ab_adapter_forward(const void* x, const void* W, const void* A, const void* 
   if (!have_device()) return AB_ERR_CUDA;
   if (N == 0) return AB_OK;
   if (!ws || !aligned(ws, 256)) return AB_ERR_WORKSPACE;
+  if (adapter_tc_supported(c, nullptr, y, T_save, nullptr, nullptr)) {
+    if (adapter_tc_ws(N, m, n, r, L) > ws_bytes) return AB_ERR_WORKSPACE;
+    return adapter_tc_forward(c, y, T_save, ws);
+  }
   const GeneralWs w = general_ws(ws, N, m, n, r, L, dt);
   if (w.bytes > ws_bytes) return AB_ERR_WORKSPACE;
   return general_forward(c, y, T_save, w);
@@ -361,12 +358,17 @@ int ab_adapter_backward(const void* x, const void* dY, const void* W, const void
     return AB_OK;
   }
   if (!ws || !aligned(ws, 256)) return AB_ERR_WORKSPACE;
-  const GeneralWs w = general_ws(ws, N, m, n, r, L, dt);
-  if (w.bytes > ws_bytes) return AB_ERR_WORKSPACE;
   if (!dX && !dA && !dB) {
+    if (ws_bytes < sizeof(int)) return AB_ERR_WORKSPACE;
     AB_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(int), c.st));
     return AB_OK;
   }
+  if (adapter_tc_supported(c, dY, dX, T_saved, dA, dB)) {
+    if (adapter_tc_ws(N, m, n, r, L) > ws_bytes) return AB_ERR_WORKSPACE;
+    return adapter_tc_backward(c, dY, T_saved, dX, dA, dB, ws);
+  }
+  const GeneralWs w = general_ws(ws, N, m, n, r, L, dt);
+  if (w.bytes > ws_bytes) return AB_ERR_WORKSPACE;
   return general_backward(c, dY, T_saved, dX, dA, dB, w);
 }
 

@@ -1,0 +1,1232 @@
+// Adapters beside a shared projection on the tensor cores (bf16 storage, fp32 accumulation): see ab_adapter.cu for the operator.
+//
+// Rows are looked at in groups of 16.  A group is uniform when all of its rows have the same adapter (or none): its products with that
+// adapter's factors go to the tensor cores, columns of an accumulator of their own.  The rows of a mixed group go row by row over the fp32
+// pipes, a few multiply-adds beside a product that is W's anyway.  So runs of rows (prompts, training groups) cost their products, single
+// tokens of many adapters cost the reading of each adapter's factors, any order works, and no row is ever multiplied with another
+// adapter's factors, not even by zero.
+//
+//   rows_kernel     T_i = s_a F_a In_i of rows in mixed groups, one row a CTA at a time
+//   project_kernel  T of uniform groups: In tile (rows) x factors of the tile's adapters
+//   wide_kernel     Out^T = W In^T + G_a T^T: 128 output features x up to 256 rows a tile.  Rows are the N side of the MMA, so a run of
+//                   groups is a range of accumulator columns: the adapter's product is a few more slabs of the reduction with fewer columns
+//   few_kernel      the same for few rows (generation): bound by the reading of W, whose reduction is cut over a cluster
+//   adapter_grad    D_a = In^T T over the 64-row slabs that have rows of a; rows of others in such a slab are cleared in shared memory
+//
+// T travels as three bf16 pieces (hi = bf16(T), mid = bf16(T - hi), lo the rest: 24 bits): the second product takes two of them (its result
+// is rounded to bf16, 2^-17 of T is lost), the gradients take all three.
+#include <cstring>
+
+#include "ab_adapter.cuh"
+#include "ab_tc_ptx.cuh"
+
+namespace ab {
+namespace {
+
+using namespace tc;
+
+constexpr int kG = 16;                    // rows of a group
+
+// ------------------------------------------------------------------------------------------------ rows and groups
+__device__ __forceinline__ int clean_id(int a, int L) { return a >= 0 && a < L ? a : -1; }
+
+// What lane l < 16 returns for group l of the 256 rows from row0: its adapter, -1 (no adapter, or no rows), -2 (mixed).  Whole warp; lanes
+// 2 l and 2 l + 1 read the group's ids.  bad: an entry that is neither an adapter nor -1.
+__device__ __forceinline__ int group_ids(const int* __restrict__ ids, int64_t N, int L, int64_t row0, int lane, bool& bad) {
+  int first = -3, same = 1;
+  bad = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int64_t row = row0 + 8 * lane + e;
+    if (row < N) {
+      const int raw = ids[row], v = clean_id(raw, L);
+      bad |= raw < -1 || raw >= L;
+      if (first == -3) first = v;
+      same &= v == first;
+    }
+  }
+  const int of = __shfl_xor_sync(0xffffffffu, first, 1), os = __shfl_xor_sync(0xffffffffu, same, 1);
+  const int one = first == -3 ? of : first;
+  int g = one == -3 ? -1 : one;
+  if (!same || !os || (first != -3 && of != -3 && first != of)) g = -2;
+  return __shfl_sync(0xffffffffu, g, (2 * lane) & 31);
+}
+
+// The three pieces of a value; what is not finite is in the first alone.
+__device__ __forceinline__ void cut(float v, bf16& hi, bf16& mid, bf16& lo) {
+  hi = __float2bfloat16_rn(v);
+  const float h = __bfloat162float(hi);
+  const float r1 = isfinite(h) ? v - h : 0.f;
+  mid = __float2bfloat16_rn(r1);
+  lo = __float2bfloat16_rn(r1 - __bfloat162float(mid));
+}
+
+__device__ __forceinline__ void dot8(const uint4& u, const float* t, float& acc) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    acc = fmaf(__uint_as_float(w[e] << 16), t[2 * e], acc);
+    acc = fmaf(__uint_as_float(w[e] & 0xffff0000u), t[2 * e + 1], acc);
+  }
+}
+
+__device__ __forceinline__ void raise(int* abort_any, int* status) {
+  *reinterpret_cast<volatile int*>(abort_any) = 1;
+  atomicExch(status, (int)AB_ERR_TIMEOUT);
+}
+
+// ------------------------------------------------------------------------------------------------ what a backward call prepares
+// Blocks 0 .. L-1: the 64-row slabs that have rows of adapter blockIdx.x, ascending, bit 31 set where not all rows of the slab are its own.
+// Blocks behind: T (fp32) cut into pieces.
+constexpr int kPrepThreads = 512;
+__global__ void __launch_bounds__(kPrepThreads)
+prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict__ list, int* __restrict__ count, int nslab, const float* __restrict__ T,
+            bf16* __restrict__ P, int r, int rp, int* status) {
+  __shared__ int warp_cnt[kPrepThreads / 32];
+  dep_wait();
+  dep_launch();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = AB_OK;
+  if ((int)blockIdx.x >= L) {
+    const int64_t step = (int64_t)(gridDim.x - L) * kPrepThreads;
+    for (int64_t i = (int64_t)(blockIdx.x - L) * kPrepThreads + threadIdx.x; i < N * rp; i += step) {
+      const int64_t row = i / rp;
+      const int k = (int)(i - row * rp);
+      bf16 h, m, l;
+      cut(k < r ? T[row * r + k] : 0.f, h, m, l);
+      bf16* p = P + row * 3 * rp + k;
+      p[0] = h; p[rp] = m; p[2 * rp] = l;
+    }
+    fence_proxy_async_all();
+    return;
+  }
+  const int a = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t* mine = list + (int64_t)a * nslab;
+  int at = 0;
+  for (int s0 = 0; s0 < nslab; s0 += kPrepThreads) {
+    const int s = s0 + threadIdx.x;
+    int any = 0, all = 1;
+    if (s < nslab) {
+      const int64_t r0 = (int64_t)s * 64;
+#pragma unroll 16
+      for (int e = 0; e < 64; ++e) {
+        const int64_t row = r0 + e;
+        const int v = row < N ? ids[row] : -1;
+        any |= v == a;
+        all &= v == a;
+      }
+    }
+    const unsigned vote = __ballot_sync(0xffffffffu, any != 0);
+    if (lane == 0) warp_cnt[warp] = __popc(vote);
+    __syncthreads();
+    int ahead = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < kPrepThreads / 32; ++w) {
+      const int c = warp_cnt[w];
+      ahead += w < warp ? c : 0;
+      sum += c;
+    }
+    if (any) mine[at + ahead + __popc(vote & ((1u << lane) - 1u))] = (uint32_t)s | (all ? 0u : 0x80000000u);
+    at += sum;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) count[a] = at;
+}
+
+// ------------------------------------------------------------------------------------------------ T of rows in mixed groups
+struct ProjParams {
+  const bf16* In; int64_t N; int K;
+  const bf16* F; int64_t strideF;           // f_mn 0: F_a is r x K, row-major; 1: K x r
+  int f_mn;
+  const float* scale; const int* ids;
+  float* T; bf16* P;                        // T: N x r; P: N x 3 rp
+  int r, rp, L;
+  int all_rows;                             // every row goes this way
+  int unit;                                 // rows of a CTA, a divisor of 16
+  int first;                                // the call's first kernel
+  int* status;
+  // project_kernel
+  int nk, tile_rows, ns, slot_bytes, in_bytes, f_bytes, q_max, tmem_cols;
+};
+
+constexpr int kRowsThreads = 256;
+
+__device__ __forceinline__ void put_T(const ProjParams& p, int64_t row, int k, float v) {
+  bf16 h, m, l;
+  cut(v, h, m, l);
+  bf16* q = p.P + row * 3 * p.rp + k;
+  q[0] = h; q[p.rp] = m; q[2 * p.rp] = l;
+  if (k < p.r) p.T[row * p.r + k] = v;
+}
+
+// A CTA has `unit` rows of one group and, where gridDim.y > 1, eight of the r values.  f_mn 0: a warp a value, lanes along K; f_mn 1:
+// a thread has eight neighbouring values and every so manieth row of F_a.
+__global__ void __launch_bounds__(kRowsThreads)
+rows_kernel(const ProjParams p) {
+  __shared__ float red[kRowsThreads / 32][32][8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (p.first) dep_wait();
+  dep_launch();
+  if (p.first && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = AB_OK;
+  const int64_t row0 = (int64_t)blockIdx.x * p.unit;
+  bool work = p.all_rows != 0;
+  if (!work) {
+    const int64_t g0 = row0 & ~(int64_t)(kG - 1);
+    const int64_t row = g0 + (lane & 15);
+    const int v = row < p.N ? clean_id(p.ids[row], p.L) : -3, v0 = __shfl_sync(0xffffffffu, v, 0);
+    work = __any_sync(0xffffffffu, v != -3 && v != v0);
+  }
+  if (work) {
+    for (int64_t row = row0; row < row0 + p.unit && row < p.N; ++row) {
+      const int a = clean_id(p.ids[row], p.L);
+      const float s = a < 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
+      const uint4* x = reinterpret_cast<const uint4*>(p.In + row * (int64_t)p.K);
+      if (a < 0) {
+        if (blockIdx.y == 0) for (int k = threadIdx.x; k < p.rp; k += kRowsThreads) put_T(p, row, k, 0.f);
+      } else if (!p.f_mn) {
+        const int stride = gridDim.y > 1 ? p.rp : 8;
+        for (int k = (int)blockIdx.y * 8 + warp; k < p.rp; k += stride) {
+          float v = 0.f;
+          if (k < p.r) {
+            const uint4* f = reinterpret_cast<const uint4*>(p.F + a * p.strideF + (int64_t)k * p.K);
+            for (int j = lane; j < p.K / 8; j += 128) {
+              uint4 u[4], w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (j + 32 * e < p.K / 8) { u[e] = f[j + 32 * e]; w[e] = x[j + 32 * e]; }
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (j + 32 * e < p.K / 8) {
+                  const uint32_t xs[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
+                  float t[8];
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) { t[2 * i] = __uint_as_float(xs[i] << 16); t[2 * i + 1] = __uint_as_float(xs[i] & 0xffff0000u); }
+                  dot8(u[e], t, v);
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+          }
+          if (lane == 0) put_T(p, row, k, s * v);
+          if (gridDim.y > 1) break;
+        }
+      } else {
+        const int oct = p.r / 8;
+        int op = 1;
+        while (op < oct) op <<= 1;                           // at most 32
+        const int o = threadIdx.x % op, f0 = threadIdx.x / op, step = kRowsThreads / op;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (o < oct) {
+          const bf16* F = p.F + a * p.strideF + 8 * o;
+          const bf16* xr = p.In + row * (int64_t)p.K;
+#pragma unroll 4
+          for (int f = f0; f < p.K; f += step) {
+            const uint4 u = *reinterpret_cast<const uint4*>(F + (int64_t)f * p.r);
+            const float xv = __bfloat162float(xr[f]);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[2 * e] = fmaf(__uint_as_float(w[e] << 16), xv, v[2 * e]);
+              v[2 * e + 1] = fmaf(__uint_as_float(w[e] & 0xffff0000u), xv, v[2 * e + 1]);
+            }
+          }
+        }
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1)
+          if (d >= op) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += __shfl_xor_sync(0xffffffffu, v[e], d);
+          }
+        if (lane < op) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) red[warp][lane][e] = v[e];
+        }
+        __syncthreads();
+        for (int k = threadIdx.x; k < p.rp; k += kRowsThreads) {
+          float t = 0.f;
+          if (k < p.r)
+            for (int w = 0; w < kRowsThreads / 32; ++w) t += red[w][k / 8][k % 8];
+          put_T(p, row, k, s * t);
+        }
+        __syncthreads();
+      }
+    }
+  }
+  fence_proxy_async_all();
+  if (!p.first) dep_wait();          // this kernel is done only after the one before it
+}
+
+// ------------------------------------------------------------------------------------------------ T of uniform groups
+constexpr int kProjTcThreads = 192;       // 0 = TMA producer, 1 = MMA issuer and TMEM owner, 2..5 = epilogue
+constexpr int kMaxStages = 8;
+struct ProjBars {
+  uint64_t full[kMaxStages], empty[kMaxStages], done, drained;
+  uint32_t tmem_base;
+  int abort_any;
+  int nad, ad[8], group[8];               // the tile's adapters, and the adapter of each of its groups
+};
+
+__global__ void __launch_bounds__(kProjTcThreads)
+project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmF, const ProjParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  ProjBars* b = reinterpret_cast<ProjBars*>(ring + (size_t)p.ns * p.slot_bytes);
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int64_t row0 = (int64_t)blockIdx.x * p.tile_rows;
+  dep_launch();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
+    mbar_init(&b->done, 1);
+    mbar_init(&b->drained, 4);
+    b->abort_any = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmIn); tma_prefetch_desc(&tmF);
+  }
+  if (warp == 0) {
+    bool bad;
+    const int g = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+    const int ng = p.tile_rows / kG;
+    int nad = 0;
+    for (int i = 0; i < ng; ++i) {
+      const int v = __shfl_sync(0xffffffffu, g, i);
+      if (lane == 0) b->group[i] = v;
+      bool seen = v < 0;
+      for (int e = 0; e < i; ++e) seen |= __shfl_sync(0xffffffffu, g, e) == v;
+      if (!seen) { if (lane == 0) b->ad[nad] = v; ++nad; }
+    }
+    if (lane == 0) b->nad = nad;
+  }
+  if (warp == 1) tmem_alloc(&b->tmem_base, p.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
+  const int nad = (int)uniform(*reinterpret_cast<volatile int*>(&b->nad));
+
+  if (warp == 0) {
+    int slot = 0, ph = 1;
+    bool ok = true;
+    for (int q0 = 0; q0 < nad && ok; q0 += p.q_max) {
+      const int q = nad - q0 < p.q_max ? nad - q0 : p.q_max;
+      for (int i = 0; i < p.nk; ++i) {
+        if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
+        if (elect_one()) {
+          uint8_t* dst = ring + (size_t)slot * p.slot_bytes;
+          uint64_t* bar = &b->full[slot];
+          mbar_arrive_expect_tx(bar, p.in_bytes + q * p.f_bytes);
+          tma_load_2d(dst, &tmIn, bar, i * 64, (int)row0);
+          for (int e = 0; e < q; ++e) {
+            uint8_t* df = dst + p.in_bytes + e * p.f_bytes;
+            const int a = b->ad[q0 + e];
+            if (p.f_mn) for (int h = 0; h * 8192 < p.f_bytes; ++h) tma_load_3d(df + h * 8192, &tmF, bar, 64 * h, i * 64, a);
+            else tma_load_3d(df, &tmF, bar, i * 64, 0, a);
+          }
+        }
+        __syncwarp();
+        if (++slot == p.ns) { slot = 0; ph ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    const uint32_t idesc = instr_desc_bf16(128, p.rp, 0, p.f_mn), base = uniform(smem_u32(ring));
+    const uint64_t dI = smem_desc_sw128(base, 16), dF = smem_desc_sw128(base + p.in_bytes, p.f_mn ? 8192 : 16);
+    const uint64_t f_step = p.f_mn ? 128u : 2u, slot_step = (uint64_t)(p.slot_bytes >> 4), q_step = (uint64_t)(p.f_bytes >> 4);
+    int slot = 0, ph = 0, pass = 0;
+    bool ok = true;
+    for (int q0 = 0; q0 < nad && ok; q0 += p.q_max, ++pass) {
+      const int q = nad - q0 < p.q_max ? nad - q0 : p.q_max;
+      if (pass > 0) {
+        if (!mbar_wait_warp(&b->drained, (pass - 1) & 1)) { raise(&b->abort_any, p.status); break; }
+        tc_fence_after();
+      }
+      for (int i = 0; i < p.nk; ++i) {
+        if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
+        tc_fence_after();
+        const uint64_t da = dI + slot_step * slot, db = dF + slot_step * slot;
+        const int ksteps = (p.K - i * 64 + 15) >> 4;
+        if (elect_one()) {
+          for (int e = 0; e < q; ++e) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              if (kk < ksteps) tc_mma_bf16(tmem + e * p.rp, da + 2 * kk, db + q_step * e + f_step * kk, idesc, (i | kk) != 0);
+          }
+          tc_commit(&b->empty[slot]);
+        }
+        __syncwarp();
+        if (++slot == p.ns) { slot = 0; ph ^= 1; }
+      }
+      if (ok && elect_one()) tc_commit(&b->done);
+      __syncwarp();
+    }
+  } else {
+    const int qw = warp & 3;                 // quarter of the TMEM lanes this warp may read = its 32 rows of the tile
+    const int lrow = qw * 32 + lane;
+    const int64_t row = row0 + lrow;
+    const bool live = lrow < p.tile_rows && row < p.N;
+    const int a = live ? b->group[lrow / kG] : -2;
+    const float s = a < 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
+    if (a == -1) {                           // no adapter: zeros
+      for (int k = 0; k < p.r; k += 4) *reinterpret_cast<float4*>(p.T + row * p.r + k) = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < 3 * p.rp; k += 8) *reinterpret_cast<uint4*>(p.P + row * 3 * p.rp + k) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    int pass = 0;
+    for (int q0 = 0; q0 < nad; q0 += p.q_max, ++pass) {
+      const int q = nad - q0 < p.q_max ? nad - q0 : p.q_max;
+      if (!mbar_wait_warp(&b->done, pass & 1)) { raise(&b->abort_any, p.status); break; }
+      tc_fence_after();
+      for (int e = 0; e < q; ++e) {
+        const bool mine = a >= 0 && a == b->ad[q0 + e];
+        if (!__any_sync(0xffffffffu, mine)) continue;
+        for (int c = 0; c < p.rp; c += 16) {
+          float v[16];
+          tmem_ld16(tmem + ((uint32_t)(qw * 32) << 16) + e * p.rp + c, v);
+          if (!mine) continue;
+          uint32_t h[8], m[8], l[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            bf16 hh[2], mm[2], ll[2];
+            v[2 * i] *= s; v[2 * i + 1] *= s;
+            cut(v[2 * i], hh[0], mm[0], ll[0]);
+            cut(v[2 * i + 1], hh[1], mm[1], ll[1]);
+            h[i] = (uint32_t)__bfloat16_as_ushort(hh[0]) | ((uint32_t)__bfloat16_as_ushort(hh[1]) << 16);
+            m[i] = (uint32_t)__bfloat16_as_ushort(mm[0]) | ((uint32_t)__bfloat16_as_ushort(mm[1]) << 16);
+            l[i] = (uint32_t)__bfloat16_as_ushort(ll[0]) | ((uint32_t)__bfloat16_as_ushort(ll[1]) << 16);
+          }
+          bf16* P = p.P + row * 3 * p.rp + c;
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            *reinterpret_cast<uint4*>(P + 8 * g) = make_uint4(h[4 * g], h[4 * g + 1], h[4 * g + 2], h[4 * g + 3]);
+            *reinterpret_cast<uint4*>(P + p.rp + 8 * g) = make_uint4(m[4 * g], m[4 * g + 1], m[4 * g + 2], m[4 * g + 3]);
+            *reinterpret_cast<uint4*>(P + 2 * p.rp + 8 * g) = make_uint4(l[4 * g], l[4 * g + 1], l[4 * g + 2], l[4 * g + 3]);
+            if (c + 8 * g < p.r) {
+              float4* t = reinterpret_cast<float4*>(p.T + row * p.r + c + 8 * g);
+              t[0] = make_float4(v[8 * g], v[8 * g + 1], v[8 * g + 2], v[8 * g + 3]);
+              t[1] = make_float4(v[8 * g + 4], v[8 * g + 5], v[8 * g + 6], v[8 * g + 7]);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b->drained);
+    }
+    fence_proxy_async_all();
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*reinterpret_cast<volatile int*>(&b->abort_any)) {
+    // give loads that are still in flight time to land before the shared memory is released
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) { }
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+  dep_wait();            // this kernel is done only after the one before it
+}
+
+// ------------------------------------------------------------------------------------------------ Out^T = W In^T + G_a T^T
+struct OutParams {
+  int64_t N; int P, K, nk;                  // rows, output features, reduction of the shared product, its slabs
+  int r, rp, L;
+  int mn;                                   // 0: W is P x K and G_a P x r; 1: W is K x P and G_a r x P
+  const int* ids; const float* T;
+  const bf16* G; int64_t strideG;
+  bf16* Out;
+  int bn, nft, ntiles, ns, slot_bytes, tmem_cols;
+  int csize;                                // few_kernel: CTAs of a cluster
+  int* status;
+};
+
+// sum_k G_a(f, k) T[k] of one row and one output feature
+__device__ __forceinline__ float small_dot(const OutParams& p, int a, int f, const float* __restrict__ T) {
+  const bf16* g = p.G + a * p.strideG;
+  float v = 0.f;
+  if (!p.mn) {
+    const uint4* q = reinterpret_cast<const uint4*>(g + (int64_t)f * p.r);
+#pragma unroll 2
+    for (int k = 0; k < p.r / 8; ++k) {
+      const uint4 u = q[k];
+      const float4 t0 = *reinterpret_cast<const float4*>(T + 8 * k), t1 = *reinterpret_cast<const float4*>(T + 8 * k + 4);
+      const float t[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
+      dot8(u, t, v);
+    }
+  } else {
+#pragma unroll 8
+    for (int k = 0; k < p.r; ++k) v = fmaf(__bfloat162float(g[(int64_t)k * p.P + f]), T[k], v);
+  }
+  return v;
+}
+
+constexpr int kWideThreads = 192;
+constexpr int kABytes = 16384;            // 128 features x 64 bf16
+struct WideBars {
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
+  uint32_t tmem_base;
+  int abort_any;
+};
+
+// The slabs of a tile behind the shared product's: for every run of groups with one adapter, piece by piece.  body(a, g0, g1, piece, j)
+// returns false to stop.
+template <typename F>
+__device__ __forceinline__ bool for_runs(int gid, int ngroups, int rp, F&& body) {
+  int g = 0;
+  while (g < ngroups) {
+    const int a = (int)uniform(__shfl_sync(0xffffffffu, gid, g));
+    if (a < 0) { ++g; continue; }
+    int e = g + 1;
+    while (e < ngroups && (int)uniform(__shfl_sync(0xffffffffu, gid, e)) == a) ++e;
+    for (int piece = 0; piece < 2; ++piece)
+      for (int j = 0; j * 64 < rp; ++j)
+        if (!body(a, g, e, piece, j)) return false;
+    g = e;
+  }
+  return true;
+}
+
+__global__ void __launch_bounds__(kWideThreads, 1)
+wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmG,
+            const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmOut, const OutParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* stg = ring + (size_t)p.ns * p.slot_bytes;              // per epilogue warp two tiles of 32 rows x 32 features
+  WideBars* b = reinterpret_cast<WideBars*>(stg + 4 * 2 * 2048);
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  dep_launch();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&b->acc_full[i], 1); mbar_init(&b->acc_empty[i], 4); }
+    b->abort_any = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmW); tma_prefetch_desc(&tmIn); tma_prefetch_desc(&tmG); tma_prefetch_desc(&tmT); tma_prefetch_desc(&tmOut);
+  }
+  if (warp == 1) tmem_alloc(&b->tmem_base, p.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
+  const int ngroups = p.bn / kG;
+  // The kernels before this one started only after all that a caller had in the stream before: x, W, the factors and the map are
+  // complete.  T alone comes from them, and is waited for where it is read.
+
+  if (warp == 0) {
+    int slot = 0, ph = 1;
+    bool ok = true, waited = false;
+    const uint32_t tx = kABytes + p.bn * 128;
+    for (int tile = blockIdx.x; tile < p.ntiles && ok; tile += gridDim.x) {
+      const int f0 = (tile % p.nft) * 128, row0 = (tile / p.nft) * p.bn;
+      bool bad;
+      const int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+      for (int i = 0; i < p.nk; ++i) {
+        if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
+        if (elect_one()) {
+          uint8_t* dst = ring + (size_t)slot * p.slot_bytes;
+          uint64_t* bar = &b->full[slot];
+          mbar_arrive_expect_tx(bar, tx);
+          if (p.mn) { tma_load_2d(dst, &tmW, bar, f0, i * 64); tma_load_2d(dst + 8192, &tmW, bar, f0 + 64, i * 64); }
+          else tma_load_2d(dst, &tmW, bar, i * 64, f0);
+          tma_load_2d(dst + kABytes, &tmIn, bar, i * 64, row0);
+        }
+        __syncwarp();
+        if (++slot == p.ns) { slot = 0; ph ^= 1; }
+      }
+      if (!ok) break;
+      if (!waited) { dep_wait(); fence_proxy_async_all(); waited = true; }
+      ok = for_runs(gid, ngroups, p.rp, [&](int a, int, int, int piece, int j) {
+        if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); return false; }
+        if (elect_one()) {
+          uint8_t* dst = ring + (size_t)slot * p.slot_bytes;
+          uint64_t* bar = &b->full[slot];
+          mbar_arrive_expect_tx(bar, tx);
+          if (p.mn) { tma_load_3d(dst, &tmG, bar, f0, j * 64, a); tma_load_3d(dst + 8192, &tmG, bar, f0 + 64, j * 64, a); }
+          else tma_load_3d(dst, &tmG, bar, j * 64, f0, a);
+          tma_load_2d(dst + kABytes, &tmT, bar, piece * p.rp + j * 64, row0);
+        }
+        __syncwarp();
+        if (++slot == p.ns) { slot = 0; ph ^= 1; }
+        return true;
+      });
+    }
+  } else if (warp == 1) {
+    int slot = 0, ph = 0, it = 0;
+    bool ok = true;
+    const uint32_t base = uniform(smem_u32(ring)), idesc = instr_desc_bf16(128, p.bn, p.mn, 0);
+    const uint64_t dA = smem_desc_sw128(base, p.mn ? 8192 : 16), dB = smem_desc_sw128(base + kABytes, 16);
+    const uint64_t a_step = p.mn ? 128u : 2u, slot_step = (uint64_t)(p.slot_bytes >> 4);
+    for (int tile = blockIdx.x; tile < p.ntiles && ok; tile += gridDim.x, ++it) {
+      const int row0 = (tile / p.nft) * p.bn, buf = it & 1;
+      bool bad;
+      const int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+      if (!mbar_wait_warp(&b->acc_empty[buf], ((it >> 1) & 1) ^ 1)) { raise(&b->abort_any, p.status); break; }
+      tc_fence_after();
+      const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1));
+      for (int i = 0; i < p.nk; ++i) {
+        if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
+        tc_fence_after();
+        const uint64_t da = dA + slot_step * slot, db = dB + slot_step * slot;
+        const int ksteps = (p.K - i * 64 + 15) >> 4;
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            if (kk < ksteps) tc_mma_bf16(tacc, da + a_step * kk, db + 2 * kk, idesc, (i | kk) != 0);
+          tc_commit(&b->empty[slot]);
+        }
+        __syncwarp();
+        if (++slot == p.ns) { slot = 0; ph ^= 1; }
+      }
+      if (!ok) break;
+      ok = for_runs(gid, ngroups, p.rp, [&](int, int g0, int g1, int, int j) {
+        if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); return false; }
+        tc_fence_after();
+        const uint64_t da = dA + slot_step * slot, db = dB + slot_step * slot + (uint64_t)(g0 * (kG * 128 >> 4));
+        const uint32_t id = instr_desc_bf16(128, (g1 - g0) * kG, p.mn, 0);
+        const int ksteps = (p.rp - j * 64 + 15) >> 4;
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            if (kk < ksteps) tc_mma_bf16(tacc + g0 * kG, da + a_step * kk, db + 2 * kk, id, 1u);
+          tc_commit(&b->empty[slot]);
+        }
+        __syncwarp();
+        if (++slot == p.ns) { slot = 0; ph ^= 1; }
+        return true;
+      });
+      if (ok && elect_one()) tc_commit(&b->acc_full[buf]);
+      __syncwarp();
+    }
+  } else {
+    const int qw = warp & 3;
+    const uint32_t lane_base = (uint32_t)(qw * 32) << 16;
+    uint8_t* my = stg + (size_t)(warp - 2) * 2 * 2048;
+    int nst = 0, it = 0;
+    bool ok = true;
+    dep_wait();                          // T is complete; and this kernel is done only after the ones before it
+    for (int tile = blockIdx.x; tile < p.ntiles && ok; tile += gridDim.x, ++it) {
+      const int f0 = (tile % p.nft) * 128 + qw * 32, row0 = (tile / p.nft) * p.bn, buf = it & 1;
+      bool bad;
+      const int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+      if (tile % p.nft == 0 && qw == 0 && __any_sync(0xffffffffu, bad && lane * 8 < p.bn) && lane == 0) atomicExch(p.status, (int)AB_ERR_INVALID_ARG);
+      const unsigned mixed = __ballot_sync(0xffffffffu, gid == -2 && lane < ngroups);
+      ok = mbar_wait_warp(&b->acc_full[buf], (it >> 1) & 1);
+      if (!ok) { raise(&b->abort_any, p.status); break; }
+      tc_fence_after();
+      const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1)) + lane_base;
+      const bool live = f0 < p.P;
+      for (int g0 = 0; g0 < ngroups; g0 += 2) {
+        uint32_t v[2][16];
+        tmem_ld16_nowait(tacc + g0 * kG, v[0]);
+        if (g0 + 1 < ngroups) tmem_ld16_nowait(tacc + g0 * kG + kG, v[1]);
+        tmem_wait_ld();
+        if (g0 + 2 >= ngroups) {         // the last columns are in registers: hand the accumulator back
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&b->acc_empty[buf]);
+        }
+        if (!live || (int64_t)row0 + g0 * kG >= p.N) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (!((mixed >> (g0 + h)) & 1u)) continue;
+          const int f = f0 + lane;
+#pragma unroll
+          for (int e = 0; e < kG; ++e) {
+            const int64_t row = (int64_t)row0 + (g0 + h) * kG + e;
+            const int a = row < p.N ? clean_id(p.ids[row], p.L) : -1;
+            if (a >= 0 && f < p.P) v[h][e] = __float_as_uint(__uint_as_float(v[h][e]) + small_dot(p, a, f, p.T + row * p.r));
+          }
+        }
+        uint8_t* tile_s = my + (nst & 1) * 2048;
+        ++nst;
+        if (lane == 0) tma_store_wait_read<1>();
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < kG; ++e)
+            *reinterpret_cast<bf16*>(tile_s + (h * kG + e) * 64 + lane * 2) = __float2bfloat16_rn(__uint_as_float(v[h][e]));
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_2d(&tmOut, tile_s, f0, row0 + g0 * kG);
+          tma_store_commit();
+        }
+      }
+    }
+    if (lane == 0) tma_store_wait_all();
+    __syncwarp();
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*reinterpret_cast<volatile int*>(&b->abort_any)) {
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) { }
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the same for few rows
+// One tile of 128 features x all rows (bn, at most 128) a cluster; its CTAs have a part of the reduction each.  Their partial sums
+// meet in the shared memory of the CTA that finishes a share of the rows, which adds them in rank order.  The adapters' part of
+// those rows is summed by the epilogue warps while W is still arriving.
+struct FewBars {
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full;
+  uint32_t tmem_base;
+  int abort_any;
+};
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+constexpr int kFewRows = 128;
+__global__ void __launch_bounds__(kWideThreads, 1)
+few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const OutParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const int share = (p.bn + p.csize - 1) / p.csize;               // rows that a CTA finishes
+  float* red = reinterpret_cast<float*>(ring + (size_t)p.ns * p.slot_bytes);      // [csize][share][128]
+  FewBars* b = reinterpret_cast<FewBars*>(red + (size_t)p.csize * share * 128);
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int ft = (int)blockIdx.x / p.csize, rank = (int)blockIdx.x - ft * p.csize, f0 = ft * 128;
+  const int per = (p.nk + p.csize - 1) / p.csize, i0 = rank * per, i1 = i0 + per < p.nk ? i0 + per : p.nk;
+  dep_launch();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
+    mbar_init(&b->acc_full, 1);
+    b->abort_any = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmW); tma_prefetch_desc(&tmIn);
+  }
+  cluster_arrive();                        // paired with the wait before the first access to another CTA's shared memory
+  if (warp == 1) tmem_alloc(&b->tmem_base, p.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
+  float acc[kG];
+
+  if (warp == 0) {
+    int slot = 0, ph = 1;
+    for (int i = i0; i < i1; ++i) {
+      if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); break; }
+      if (elect_one()) {
+        uint8_t* dst = ring + (size_t)slot * p.slot_bytes;
+        uint64_t* bar = &b->full[slot];
+        mbar_arrive_expect_tx(bar, kABytes + p.bn * 128);
+        if (p.mn) { tma_load_2d(dst, &tmW, bar, f0, i * 64); tma_load_2d(dst + 8192, &tmW, bar, f0 + 64, i * 64); }
+        else tma_load_2d(dst, &tmW, bar, i * 64, f0);
+        tma_load_2d(dst + kABytes, &tmIn, bar, i * 64, 0);
+      }
+      __syncwarp();
+      if (++slot == p.ns) { slot = 0; ph ^= 1; }
+    }
+  } else if (warp == 1) {
+    const uint32_t base = uniform(smem_u32(ring)), idesc = instr_desc_bf16(128, p.bn, p.mn, 0);
+    const uint64_t dA = smem_desc_sw128(base, p.mn ? 8192 : 16), dB = smem_desc_sw128(base + kABytes, 16);
+    const uint64_t a_step = p.mn ? 128u : 2u, slot_step = (uint64_t)(p.slot_bytes >> 4);
+    int slot = 0, ph = 0;
+    for (int i = i0; i < i1; ++i) {
+      if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); break; }
+      tc_fence_after();
+      const uint64_t da = dA + slot_step * slot, db = dB + slot_step * slot;
+      const int ksteps = (p.K - i * 64 + 15) >> 4;
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          if (kk < ksteps) tc_mma_bf16(tmem, da + a_step * kk, db + 2 * kk, idesc, (i > i0 || kk) ? 1u : 0u);
+        tc_commit(&b->empty[slot]);
+      }
+      __syncwarp();
+      if (++slot == p.ns) { slot = 0; ph ^= 1; }
+    }
+    if (elect_one()) tc_commit(&b->acc_full);
+    __syncwarp();
+  }
+  const int qw = warp & 3, f = f0 + qw * 32 + lane, t0 = rank * share;
+  bool ok = true;
+  if (warp >= 2) {
+    dep_wait();                            // T is complete
+    if (ft == 0 && rank == 0 && warp == 2) {
+      bool bad = false;
+      for (int t = lane; t < p.N; t += 32) bad |= p.ids[t] < -1 || p.ids[t] >= p.L;
+      if (__any_sync(0xffffffffu, bad) && lane == 0) atomicExch(p.status, (int)AB_ERR_INVALID_ARG);
+    }
+#pragma unroll
+    for (int e = 0; e < kG; ++e) {
+      const int t = t0 + e;
+      const int a = e < share && t < p.N ? clean_id(p.ids[t], p.L) : -1;
+      acc[e] = a >= 0 && f < p.P ? small_dot(p, a, f, p.T + (int64_t)t * p.r) : 0.f;
+    }
+    ok = mbar_wait_warp(&b->acc_full, 0);
+    if (!ok) raise(&b->abort_any, p.status);
+  }
+  cluster_wait();                          // every CTA of the cluster runs
+  if (warp >= 2) {
+    tc_fence_after();
+    const uint32_t dst = smem_u32(red) + (uint32_t)((rank * share * 128 + qw * 32 + lane) * 4);
+    for (int c = 0; c < p.bn; c += kG) {
+      float v[kG];
+      if (ok && i1 > i0) tmem_ld16(tmem + ((uint32_t)(qw * 32) << 16) + c, v);
+      else {
+#pragma unroll
+        for (int e = 0; e < kG; ++e) v[e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < kG; ++e) {
+        const int t = c + e, owner = t / share;
+        const uint32_t to = cluster_addr(dst + (uint32_t)((t - owner * share) * 512), owner);
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v[e]) : "memory");
+      }
+    }
+    tc_fence_before();
+  }
+  cluster_arrive();
+  cluster_wait();                          // and has written its sums
+  if (warp >= 2 && f < p.P) {
+    for (int e0 = 0; e0 < share; e0 += kG) {
+#pragma unroll
+      for (int e = 0; e < kG; ++e) {
+        const int t = t0 + e0 + e;
+        if (e0 + e >= share || t >= p.N) continue;
+        float v = 0.f;
+        for (int q = 0; q < p.csize; ++q) v += red[(q * share + e0 + e) * 128 + qw * 32 + lane];
+        float d = acc[e];
+        if (e0 > 0) {
+          const int a = clean_id(p.ids[t], p.L);
+          d = a >= 0 ? small_dot(p, a, f, p.T + (int64_t)t * p.r) : 0.f;
+        }
+        p.Out[(int64_t)t * p.P + f] = __float2bfloat16_rn(v + d);
+      }
+    }
+  }
+  __syncthreads();
+  if (*reinterpret_cast<volatile int*>(&b->abort_any)) {
+    const uint64_t w0 = globaltimer_ns();
+    while (globaltimer_ns() - w0 < 200000ull) { }
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ gradients of the factors
+struct GradJob { int P, tiles; float* out; int64_t strideO, o_f, o_k, slice_stride; };
+struct GradParams {
+  GradJob job[2];
+  int64_t N; int r, rp, L, nslab;
+  int halves;                               // parts of the r values a CTA has one of (128 each)
+  int slices;
+  int stacked;                              // the three pieces side by side as columns of one MMA
+  int nb;                                   // 64-column boxes of the small operand a slab
+  int ns, slot_bytes, tmem_cols;
+  const int* ids; const uint32_t* list; const int* count;
+  int check;                                // report bad map entries (no other kernel of the call does)
+  int* status;
+};
+constexpr int kFlush = 8;                 // slabs (512 rows) a TMEM accumulator takes before it is added to fp32 registers: the tensor
+                                          // cores cut off what does not fit a sum, registers round
+struct GradBars {
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
+  uint32_t tmem_base;
+  int abort_any;
+};
+
+template <int kChunks>                    // up to 16 kChunks values of r a CTA
+__global__ void __launch_bounds__(kWideThreads, 1)
+adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_constant__ CUtensorMap tmS0,
+                       const __grid_constant__ CUtensorMap tmAct1, const __grid_constant__ CUtensorMap tmS1, const GradParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  GradBars* b = reinterpret_cast<GradBars*>(ring + (size_t)p.ns * p.slot_bytes);
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  int item = blockIdx.x;
+  const int slice = item % p.slices; item /= p.slices;
+  const int half = item % p.halves; item /= p.halves;
+  const int tiles = p.job[0].tiles + p.job[1].tiles;
+  int tile = item % tiles;
+  const int a = item / tiles, j = tile < p.job[0].tiles ? 0 : 1;
+  if (j) tile -= p.job[0].tiles;
+  const int f0 = tile * 128, kc0 = half * 128, kcols = p.rp - kc0 < 128 ? p.rp - kc0 : 128;
+  const CUtensorMap* tmA = j ? &tmAct1 : &tmAct0;
+  const CUtensorMap* tmS = j ? &tmS1 : &tmS0;
+  const int pieces = p.stacked ? 1 : 3;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&b->acc_full[i], 1); mbar_init(&b->acc_empty[i], 4); }
+    b->abort_any = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(tmA); tma_prefetch_desc(tmS);
+  }
+  dep_wait();
+  if (warp == 1) tmem_alloc(&b->tmem_base, p.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  dep_launch();
+  const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
+  const int cnt = (int)uniform(p.count[a]), per = (cnt + p.slices - 1) / p.slices;
+  const int e0 = slice * per < cnt ? slice * per : cnt, e1 = e0 + per < cnt ? e0 + per : cnt;
+  const uint32_t* list = p.list + (int64_t)a * p.nslab;
+  if (p.check && blockIdx.x == 0) {
+    bool bad = false;
+    for (int64_t i = threadIdx.x; i < p.N; i += kWideThreads) bad |= p.ids[i] < -1 || p.ids[i] >= p.L;
+    if (bad) atomicExch(p.status, (int)AB_ERR_INVALID_ARG);
+  }
+
+  if (warp == 0) {
+    fence_proxy_async_all();               // the pieces were written by plain stores
+    int slot = 0, ph = 1;
+    bool ok = true;
+    const uint32_t tx = kABytes + p.nb * 8192;
+    for (int e = e0; e < e1 && ok; ++e) {
+      const int row0 = (int)(uniform(list[e]) & 0x7fffffffu) * 64;
+      for (int q = 0; q < pieces; ++q) {
+        if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
+        if (elect_one()) {
+          uint8_t* dst = ring + (size_t)slot * p.slot_bytes;
+          uint64_t* bar = &b->full[slot];
+          mbar_arrive_expect_tx(bar, tx);
+          tma_load_2d(dst, tmA, bar, f0, row0);
+          tma_load_2d(dst + 8192, tmA, bar, f0 + 64, row0);
+          for (int h = 0; h < p.nb; ++h) tma_load_2d(dst + kABytes + h * 8192, tmS, bar, (p.stacked ? 0 : q * p.rp + kc0) + 64 * h, row0);
+        }
+        __syncwarp();
+        if (++slot == p.ns) { slot = 0; ph ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    const uint32_t base = uniform(smem_u32(ring)), idesc = instr_desc_bf16(128, p.stacked ? 3 * p.rp : kcols, 1, 1);
+    const uint64_t dA = smem_desc_sw128(base, 8192), dS = smem_desc_sw128(base + kABytes, 8192), slot_step = (uint64_t)(p.slot_bytes >> 4);
+    int slot = 0, ph = 0;
+    bool ok = true;
+    for (int e = e0, n = 0; e < e1 && ok; ++e, ++n) {
+      const uint32_t entry = uniform(list[e]);
+      const int flush = n / kFlush, buf = flush & 1, in = n % kFlush;
+      const bool others = entry >> 31;
+      if (in == 0) {
+        if (!mbar_wait_warp(&b->acc_empty[buf], ((flush >> 1) & 1) ^ 1)) { raise(&b->abort_any, p.status); break; }
+        tc_fence_after();
+      }
+      const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1));
+      for (int q = 0; q < pieces; ++q) {
+        if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
+        if (others) {
+          // rows that are not this adapter's: cleared in both operands, whatever they hold
+          const int64_t row = (int64_t)(entry & 0x7fffffffu) * 64 + lane;
+          const unsigned lo = __ballot_sync(0xffffffffu, row < p.N && p.ids[row] == a);
+          const unsigned hi = __ballot_sync(0xffffffffu, row + 32 < p.N && p.ids[row + 32] == a);
+          uint8_t* s = ring + (size_t)slot * p.slot_bytes;
+          for (int r4 = 0; r4 < 64; r4 += 4) {
+            const int rr = r4 + (lane >> 3);
+            const bool mine = ((rr < 32 ? lo >> rr : hi >> (rr - 32)) & 1u) != 0;
+            if (!mine)
+              for (int h = 0; h < 2 + p.nb; ++h)
+                *reinterpret_cast<uint4*>(s + h * 8192 + rr * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        const uint64_t da = dA + slot_step * slot, ds = dS + slot_step * slot;
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) tc_mma_bf16(tacc, da + 128 * kk, ds + 128 * kk, idesc, (in | q | kk) != 0);
+          tc_commit(&b->empty[slot]);
+        }
+        __syncwarp();
+        if (++slot == p.ns) { slot = 0; ph ^= 1; }
+      }
+      if (ok && (in == kFlush - 1 || e + 1 == e1) && elect_one()) tc_commit(&b->acc_full[buf]);
+      __syncwarp();
+    }
+  } else {
+    const int qw = warp & 3, f = f0 + qw * 32 + lane;
+    const uint32_t lane_base = (uint32_t)(qw * 32) << 16;
+    float R[kChunks][16];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) R[c][i] = 0.f;
+    const int flushes = (e1 - e0 + kFlush - 1) / kFlush;
+    bool ok = true;
+    for (int n = 0; n < flushes && ok; ++n) {
+      const int buf = n & 1;
+      ok = mbar_wait_warp(&b->acc_full[buf], (n >> 1) & 1);
+      if (!ok) { raise(&b->abort_any, p.status); break; }
+      tc_fence_after();
+      const uint32_t t = tmem + (uint32_t)(buf * (p.tmem_cols >> 1)) + lane_base;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        if (16 * c >= kcols) continue;
+        uint32_t u[3][16];
+        tmem_ld16_nowait(t + 16 * c, u[0]);
+        if (p.stacked) { tmem_ld16_nowait(t + p.rp + 16 * c, u[1]); tmem_ld16_nowait(t + 2 * p.rp + 16 * c, u[2]); }
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float v = __uint_as_float(u[0][i]);
+          if (p.stacked) v += __uint_as_float(u[1][i]) + __uint_as_float(u[2][i]);
+          R[c][i] += v;
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b->acc_empty[buf]);
+    }
+    const GradJob& J = p.job[j];
+    if (f < J.P) {
+      float* out = J.out + slice * J.slice_stride + a * J.strideO + (int64_t)f * J.o_f;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        if (16 * c >= kcols) continue;
+        const int k = kc0 + 16 * c;
+        if (J.o_k == 1) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            if (k + i < p.r) *reinterpret_cast<float4*>(out + k + i) = make_float4(R[c][i], R[c][i + 1], R[c][i + 2], R[c][i + 3]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (k + i < p.r) out[(int64_t)(k + i) * J.o_k] = R[c][i];
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*reinterpret_cast<volatile int*>(&b->abort_any)) {
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) { }
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, p.tmem_cols);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+int pad16(int r) { return (r + 15) / 16 * 16; }
+int pow2_cols(int c) { int v = 32; while (v < c) v <<= 1; return v; }
+
+// the stride of a lone matrix may be anything
+int stack_map(CUtensorMap* m, const AdapterCall& c, const void* F, int rows, int cols, int64_t stride, int box_rows) {
+  return make_tensor_map_stack(m, F, c.L, rows, cols, c.L > 1 ? stride : (int64_t)rows * cols, box_rows);
+}
+
+// T = s F In of all rows (two launches, or one for few rows); `first`: nothing of the call was launched before
+int launch_project(const AdapterCall& c, const void* In, int K, const void* F, int64_t strideF, bool f_mn, float* T, bf16* P, bool first, int* status) {
+  ProjParams p;
+  std::memset(&p, 0, sizeof(p));
+  const int rp = pad16(c.r);
+  p.In = static_cast<const bf16*>(In); p.N = c.N; p.K = K; p.F = static_cast<const bf16*>(F); p.strideF = strideF; p.f_mn = f_mn ? 1 : 0;
+  p.scale = c.scale; p.ids = c.ids; p.T = T; p.P = P; p.r = c.r; p.rp = rp; p.L = c.L; p.first = first ? 1 : 0; p.status = status;
+  p.all_rows = c.N <= 64 ? 1 : 0;
+  p.unit = c.N <= 1024 ? 1 : c.N <= 8192 ? 4 : 16;
+  const int64_t units = (c.N + p.unit - 1) / p.unit;
+  const int ky = !f_mn && units <= 256 ? (rp + 7) / 8 : 1;
+  AB_TRY(launch_after(rows_kernel, dim3((unsigned)units, (unsigned)ky), (unsigned)kRowsThreads, 0, 1, c.st, p));
+  if (p.all_rows) return AB_OK;
+  p.nk = (K + 63) / 64;
+  p.tile_rows = c.N > (int64_t)64 * 2 * sm_count() ? 128 : 64;
+  p.in_bytes = p.tile_rows * 128;
+  p.f_bytes = f_mn ? (c.r + 63) / 64 * 8192 : rp * 128;
+  const int room = p.f_bytes > 8192 ? p.f_bytes : 8192;
+  p.q_max = room / p.f_bytes < 512 / rp ? room / p.f_bytes : 512 / rp;
+  if (p.q_max > 8) p.q_max = 8;
+  p.slot_bytes = p.in_bytes + room;
+  if (p.slot_bytes < 16384) p.slot_bytes = 16384;          // an MMA reads 128 rows of In, loaded or not
+  p.ns = 100 * 1024 / p.slot_bytes < kMaxStages ? 100 * 1024 / p.slot_bytes : kMaxStages;
+  if (p.ns < 3) p.ns = 3;
+  p.tmem_cols = pow2_cols(p.q_max * rp);
+  CUtensorMap tmIn, tmF;
+  AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.tile_rows));
+  AB_TRY(stack_map(&tmF, c, F, f_mn ? K : c.r, f_mn ? c.r : K, strideF, f_mn ? 64 : rp));
+  const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + sizeof(ProjBars);
+  AB_CUDA_OK(allow_smem(project_tc_kernel));
+  return launch_after(project_tc_kernel, (unsigned)((c.N + p.tile_rows - 1) / p.tile_rows), (unsigned)kProjTcThreads, smem, 1, c.st, tmIn, tmF, p);
+}
+
+// Out = In W^T + T G^T; mn as in OutParams
+int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void* G, int64_t strideG, void* Out, int P, const float* T, const bf16* Tp,
+               int* status) {
+  const int sms = sm_count();
+  if (sms <= 0) return AB_ERR_CUDA;
+  OutParams p;
+  std::memset(&p, 0, sizeof(p));
+  const int rp = pad16(c.r);
+  p.N = c.N; p.P = P; p.K = K; p.nk = (K + 63) / 64; p.r = c.r; p.rp = rp; p.L = c.L; p.mn = mn ? 1 : 0; p.ids = c.ids; p.T = T;
+  p.G = static_cast<const bf16*>(G); p.strideG = strideG; p.Out = static_cast<bf16*>(Out); p.status = status;
+  p.nft = (P + 127) / 128;
+  CUtensorMap tmW, tmIn, tmG, tmT, tmOut;
+  if (mn) AB_TRY(make_tensor_map_2d(&tmW, c.W, false, K, P, P, 64, 64));
+  else AB_TRY(make_tensor_map_2d(&tmW, c.W, false, P, K, K, 64, 128));
+  if (c.N <= kFewRows) {
+    p.bn = (int)((c.N + 15) / 16 * 16);
+    p.csize = 8;
+    while (p.csize > 1 && (p.nft * p.csize > sms || 2 * p.csize > p.nk)) p.csize >>= 1;
+    p.slot_bytes = kABytes + p.bn * 128;
+    const int share = (p.bn + p.csize - 1) / p.csize;
+    const size_t red = (size_t)p.csize * share * 512;
+    p.ns = (int)((kMaxSmem - 2048 - red - sizeof(FewBars)) / p.slot_bytes);
+    if (p.ns > kMaxStages) p.ns = kMaxStages;
+    p.tmem_cols = pow2_cols(p.bn);
+    AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn));
+    AB_CUDA_OK(allow_smem(few_kernel));
+    return launch_after(few_kernel, (unsigned)(p.nft * p.csize), (unsigned)kWideThreads, 1024 + (size_t)p.ns * p.slot_bytes + red + sizeof(FewBars),
+                        p.csize, c.st, tmW, tmIn, p);
+  }
+  // rows of a tile: cycles of the busiest SM, a slab's operands arriving at 64 bytes a cycle or its MMAs, whichever is longer
+  double best = 1e30;
+  for (int bn = 32; bn <= 256; bn *= 2) {
+    const int64_t tiles = (int64_t)p.nft * ((c.N + bn - 1) / bn);
+    const double slab = 2.0 * (128 + bn) > (bn <= 64 ? 300.0 : bn <= 128 ? 330.0 : 560.0) ? 2.0 * (128 + bn) : bn <= 64 ? 300.0 : bn <= 128 ? 330.0 : 560.0;
+    const double t = (double)((tiles + sms - 1) / sms) * (p.nk + 2) * slab + 3000.0;
+    if (t < best) { best = t; p.bn = bn; }
+  }
+  const int64_t tiles = (int64_t)p.nft * ((c.N + p.bn - 1) / p.bn);
+  if (tiles > 0x7fffffffll) return AB_ERR_UNSUPPORTED;
+  p.ntiles = (int)tiles;
+  p.slot_bytes = kABytes + p.bn * 128;
+  p.ns = 196608 / p.slot_bytes < kMaxStages ? 196608 / p.slot_bytes : kMaxStages;
+  p.tmem_cols = 2 * pow2_cols(p.bn);
+  AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn));
+  AB_TRY(make_tensor_map_2d(&tmT, Tp, false, (uint64_t)c.N, 3 * rp, 3 * rp, 64, p.bn));
+  AB_TRY(stack_map(&tmG, c, G, mn ? c.r : P, mn ? P : c.r, strideG, mn ? 64 : 128));
+  AB_TRY(make_tensor_map_plain(&tmOut, Out, (uint64_t)c.N, P, 32, 32));
+  AB_CUDA_OK(allow_smem(wide_kernel));
+  const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + 4 * 2 * 2048 + sizeof(WideBars);
+  return launch_after(wide_kernel, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideThreads, smem, 1, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
+}
+
+// Slices of an adapter's rows, so that there are CTAs for every SM where adapters and tiles are few
+int grad_slices(int64_t N, int m, int n, int r, int L) {
+  const int sms = sm_count() > 0 ? sm_count() : 148;
+  const int64_t items = (int64_t)L * ((m + 127) / 128 + (n + 127) / 128) * (pad16(r) > 128 ? 2 : 1);
+  const int64_t slabs = (N + 63) / 64 / L;
+  int64_t s = sms / items;
+  if (s > slabs / 8) s = slabs / 8;
+  return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+}
+
+struct TcWs { int* status; float *T, *U; bf16 *TP, *UP; uint32_t* list; int* count; float *pA, *pB; int slices, nslab; size_t bytes; };
+TcWs tc_ws(void* ws, int64_t N, int m, int n, int r, int L) {
+  Arena ar(ws, 0);
+  TcWs w;
+  const int rp = pad16(r);
+  w.status = ar.take_n<int>(64);
+  w.T = ar.take_n<float>((size_t)N * r);
+  w.U = ar.take_n<float>((size_t)N * r);
+  w.TP = ar.take_n<bf16>((size_t)N * 3 * rp);
+  w.UP = ar.take_n<bf16>((size_t)N * 3 * rp);
+  w.nslab = (int)((N + 63) / 64);
+  w.list = ar.take_n<uint32_t>((size_t)L * w.nslab);
+  w.count = ar.take_n<int>((size_t)L);
+  w.slices = grad_slices(N, m, n, r, L);
+  w.pA = w.slices > 1 ? ar.take_n<float>((size_t)w.slices * L * m * r) : nullptr;
+  w.pB = w.slices > 1 ? ar.take_n<float>((size_t)w.slices * L * n * r) : nullptr;
+  w.bytes = align_up(ar.used, 256);
+  return w;
+}
+
+int launch_grads(const AdapterCall& c, const void* dY, float* dA, float* dB, const TcWs& w, bool check) {
+  GradParams p;
+  std::memset(&p, 0, sizeof(p));
+  const int rp = pad16(c.r);
+  p.N = c.N; p.r = c.r; p.rp = rp; p.L = c.L; p.nslab = w.nslab; p.slices = w.slices; p.ids = c.ids; p.list = w.list; p.count = w.count;
+  p.status = w.status; p.check = check ? 1 : 0;
+  p.halves = rp > 128 ? 2 : 1;
+  p.stacked = 3 * rp <= 256 ? 1 : 0;
+  p.nb = p.stacked ? (3 * rp + 63) / 64 : ((rp < 128 ? rp : 128) + 63) / 64;
+  p.slot_bytes = kABytes + p.nb * 8192;
+  p.ns = 200 * 1024 / p.slot_bytes < kMaxStages ? 200 * 1024 / p.slot_bytes : kMaxStages;
+  p.tmem_cols = 2 * pow2_cols(p.stacked ? 3 * rp : rp < 128 ? rp : 128);
+  CUtensorMap act[2], small[2];
+  int nj = 0;
+  if (dA) {
+    AB_TRY(make_tensor_map_2d(&act[nj], dY, false, (uint64_t)c.N, c.m, c.m, 64, 64));
+    AB_TRY(make_tensor_map_2d(&small[nj], w.TP, false, (uint64_t)c.N, 3 * rp, 3 * rp, 64, 64));
+    p.job[nj] = GradJob{c.m, (c.m + 127) / 128, w.slices > 1 ? w.pA : dA, (int64_t)c.m * c.r, c.r, 1, (int64_t)c.L * c.m * c.r};
+    ++nj;
+  }
+  if (dB) {
+    AB_TRY(make_tensor_map_2d(&act[nj], c.x, false, (uint64_t)c.N, c.n, c.n, 64, 64));
+    AB_TRY(make_tensor_map_2d(&small[nj], w.UP, false, (uint64_t)c.N, 3 * rp, 3 * rp, 64, 64));
+    p.job[nj] = GradJob{c.n, (c.n + 127) / 128, w.slices > 1 ? w.pB : dB, (int64_t)c.r * c.n, 1, c.n, (int64_t)c.L * c.r * c.n};
+    ++nj;
+  }
+  if (nj == 1) { act[1] = act[0]; small[1] = small[0]; }
+  const int64_t grid = (int64_t)c.L * (p.job[0].tiles + p.job[1].tiles) * p.halves * p.slices;
+  if (grid > 0x7fffffffll) return AB_ERR_UNSUPPORTED;
+  const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + sizeof(GradBars);
+  if (rp <= 64) {
+    AB_CUDA_OK(allow_smem(adapter_grad_tc_kernel<4>));
+    AB_TRY(launch_after(adapter_grad_tc_kernel<4>, (unsigned)grid, (unsigned)kWideThreads, smem, 1, c.st, act[0], small[0], act[1], small[1], p));
+  } else {
+    AB_CUDA_OK(allow_smem(adapter_grad_tc_kernel<8>));
+    AB_TRY(launch_after(adapter_grad_tc_kernel<8>, (unsigned)grid, (unsigned)kWideThreads, smem, 1, c.st, act[0], small[0], act[1], small[1], p));
+  }
+  if (w.slices > 1) {
+    const int64_t ea = (int64_t)c.L * c.m * c.r, eb = (int64_t)c.L * c.n * c.r;
+    if (dA) AB_TRY(sum_slices(w.pA, dA, ea, ea, w.slices, c.st));
+    if (dB) AB_TRY(sum_slices(w.pB, dB, eb, eb, w.slices, c.st));
+  }
+  return AB_OK;
+}
+
+}  // namespace
+
+bool adapter_tc_shape_ok(int64_t N, int m, int n, int r, int L, int dt) {
+  return dt == AB_BF16 && m % 8 == 0 && n % 8 == 0 && r % 8 == 0 && r <= 256 && N <= ((int64_t)1 << 30);
+}
+
+bool adapter_tc_supported(const AdapterCall& c, const void* dY, const void* out, const float* T, const float* dA, const float* dB) {
+  if (!adapter_tc_shape_ok(c.N, c.m, c.n, c.r, c.L, c.dt)) return false;
+  if (c.L > 1 && (c.strideA % 8 != 0 || c.strideB % 8 != 0)) return false;
+  return aligned(c.x, 16) && aligned(c.W, 16) && aligned(c.A, 16) && aligned(c.B, 16) && aligned(dY, 16) && aligned(out, 16) && aligned(T, 16) &&
+         aligned(dA, 16) && aligned(dB, 16) && tc_device_ok();
+}
+
+size_t adapter_tc_ws(int64_t N, int m, int n, int r, int L) { return tc_ws(nullptr, N, m, n, r, L).bytes; }
+
+int adapter_tc_forward(const AdapterCall& c, void* y, float* T_save, void* ws) {
+  const TcWs w = tc_ws(ws, c.N, c.m, c.n, c.r, c.L);
+  float* T = T_save ? T_save : w.T;
+  AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, T, w.TP, true, w.status));
+  return launch_out(c, c.x, c.n, false, c.A, c.strideA, y, c.m, T, w.TP, w.status);
+}
+
+int adapter_tc_backward(const AdapterCall& c, const void* dY, const float* T_saved, void* dX, float* dA, float* dB, void* ws) {
+  const TcWs w = tc_ws(ws, c.N, c.m, c.n, c.r, c.L);
+  bool first = true;
+  if (dA || dB) {
+    const int64_t rows = dA && T_saved ? c.N : 0;
+    int64_t blocks = (rows * pad16(c.r) + kPrepThreads * 4 - 1) / (kPrepThreads * 4);
+    if (blocks > 1024) blocks = 1024;
+    AB_TRY(launch_after(prep_kernel, (unsigned)(c.L + blocks), (unsigned)kPrepThreads, 0, 1, c.st, c.ids, c.N, c.L, w.list, w.count, w.nslab, T_saved, w.TP,
+                        c.r, pad16(c.r), w.status));
+    first = false;
+  }
+  if (dX || dB) {
+    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, w.UP, first, w.status));
+    first = false;
+  }
+  if (dA && !T_saved) AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, w.TP, first, w.status));
+  if (dX) AB_TRY(launch_out(c, dY, c.m, true, c.B, c.strideB, dX, c.n, w.U, w.UP, w.status));
+  if (dA || dB) AB_TRY(launch_grads(c, dY, dA, dB, w, !dX));
+  return AB_OK;
+}
+
+}  // namespace ab

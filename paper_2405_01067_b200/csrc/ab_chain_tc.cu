@@ -1266,6 +1266,32 @@ int make_tensor_map_nhwc(CUtensorMap* m, const void* ptr, uint64_t B, uint64_t H
   return rc == CUDA_SUCCESS ? AB_OK : AB_ERR_CUDA;
 }
 
+int make_tensor_map_stack(CUtensorMap* m, const void* ptr, uint64_t count, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return AB_ERR_CUDA;
+  cuuint64_t dims[3] = {cols, rows, count};
+  cuuint64_t strides[2] = {cols * 2, stride * 2};
+  cuuint32_t box[3] = {64, box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult rc = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return rc == CUDA_SUCCESS ? AB_OK : AB_ERR_CUDA;
+}
+
+int make_tensor_map_plain(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return AB_ERR_CUDA;
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {cols * 2};
+  cuuint32_t box[2] = {box_cols, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult rc = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return rc == CUDA_SUCCESS ? AB_OK : AB_ERR_CUDA;
+}
+
 bool tc_device_ok() { return device_is_sm100() && encode_fn() != nullptr; }
 
 bool chain_tc_supported(int64_t N, int m, int n, int r, int ldA, int ldB, int dt,

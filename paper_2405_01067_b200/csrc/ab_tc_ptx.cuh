@@ -62,6 +62,8 @@ __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;"
 __device__ __forceinline__ void dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void fence_barrier_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// Orders global memory written (or to be read) by plain accesses with TMA accesses to it.
+__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 __device__ __forceinline__ void named_bar_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
@@ -76,6 +78,14 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uin
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
           smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
+      : "memory");
+}
+// 3-D tile load (matrix c2 of a stack: c0 = element along the contiguous dimension, c1 = row).
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+          smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
 // 4-D tile load (an NHWC activation: c0 = channel, c1 = x, c2 = y, c3 = image).  Coordinates may start outside
@@ -202,5 +212,10 @@ int make_tensor_map_2d(CUtensorMap* m, const void* ptr, bool f32, uint64_t rows,
 // 4-D tensor map of a bf16 NHWC activation [B, H, W, C] (C contiguous), boxes of 64 channels x bw x bh x bb.
 int make_tensor_map_nhwc(CUtensorMap* m, const void* ptr, uint64_t B, uint64_t H, uint64_t W, uint64_t C,
                          uint32_t bw, uint32_t bh, uint32_t bb);
+// 3-D tensor map of a stack of bf16 matrices [count x rows x cols], row stride cols, matrices `stride` elements apart; boxes of 64 columns x
+// box_rows of one matrix with the 128-byte swizzle.
+int make_tensor_map_stack(CUtensorMap* m, const void* ptr, uint64_t count, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows);
+// 2-D map of a row-major bf16 matrix without gaps for stores of box_cols x box_rows from unswizzled shared memory.
+int make_tensor_map_plain(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows);
 bool tc_device_ok();
 }  // namespace ab
