@@ -61,6 +61,23 @@ __device__ __forceinline__ void cut(float v, bf16& hi, bf16& mid, bf16& lo) {
   lo = __float2bfloat16_rn(r1 - __bfloat162float(mid));
 }
 
+// eight neighbouring values as pieces at P, P + rp, P + 2 rp
+__device__ __forceinline__ void put_pieces(bf16* P, int rp, const float* v) {
+  uint32_t h[4], m[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    bf16 hh[2], mm[2], ll[2];
+    cut(v[2 * i], hh[0], mm[0], ll[0]);
+    cut(v[2 * i + 1], hh[1], mm[1], ll[1]);
+    h[i] = (uint32_t)__bfloat16_as_ushort(hh[0]) | ((uint32_t)__bfloat16_as_ushort(hh[1]) << 16);
+    m[i] = (uint32_t)__bfloat16_as_ushort(mm[0]) | ((uint32_t)__bfloat16_as_ushort(mm[1]) << 16);
+    l[i] = (uint32_t)__bfloat16_as_ushort(ll[0]) | ((uint32_t)__bfloat16_as_ushort(ll[1]) << 16);
+  }
+  *reinterpret_cast<uint4*>(P) = make_uint4(h[0], h[1], h[2], h[3]);
+  *reinterpret_cast<uint4*>(P + rp) = make_uint4(m[0], m[1], m[2], m[3]);
+  *reinterpret_cast<uint4*>(P + 2 * rp) = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
 __device__ __forceinline__ void dot8(const uint4& u, const float* t, float& acc) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -77,7 +94,7 @@ __device__ __forceinline__ void raise(int* abort_any, int* status) {
 
 // ------------------------------------------------------------------------------------------------ what a backward call prepares
 // Blocks 0 .. L-1: the 64-row slabs that have rows of adapter blockIdx.x, ascending, bit 31 set where not all rows of the slab are its own.
-// Blocks behind: T (fp32) cut into pieces.
+// Blocks behind: T (fp32) cut into pieces, eight values a thread.
 constexpr int kPrepThreads = 512;
 __global__ void __launch_bounds__(kPrepThreads)
 prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict__ list, int* __restrict__ count, int nslab, const float* __restrict__ T,
@@ -88,13 +105,16 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict_
   if (blockIdx.x == 0 && threadIdx.x == 0) *status = AB_OK;
   if ((int)blockIdx.x >= L) {
     const int64_t step = (int64_t)(gridDim.x - L) * kPrepThreads;
-    for (int64_t i = (int64_t)(blockIdx.x - L) * kPrepThreads + threadIdx.x; i < N * rp; i += step) {
-      const int64_t row = i / rp;
-      const int k = (int)(i - row * rp);
-      bf16 h, m, l;
-      cut(k < r ? T[row * r + k] : 0.f, h, m, l);
-      bf16* p = P + row * 3 * rp + k;
-      p[0] = h; p[rp] = m; p[2 * rp] = l;
+    const int oct = rp / 8;
+    for (int64_t i = (int64_t)(blockIdx.x - L) * kPrepThreads + threadIdx.x; i < N * oct; i += step) {
+      const int64_t row = i / oct;
+      const int k = (int)(i - row * oct) * 8;
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (k < r) {
+        const float4 t0 = *reinterpret_cast<const float4*>(T + row * r + k), t1 = *reinterpret_cast<const float4*>(T + row * r + k + 4);
+        v[0] = t0.x; v[1] = t0.y; v[2] = t0.z; v[3] = t0.w; v[4] = t1.x; v[5] = t1.y; v[6] = t1.z; v[7] = t1.w;
+      }
+      put_pieces(P + row * 3 * rp + k, rp, v);
     }
     fence_proxy_async_all();
     return;
@@ -103,19 +123,17 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict_
   uint32_t* mine = list + (int64_t)a * nslab;
   int at = 0;
   for (int s0 = 0; s0 < nslab; s0 += kPrepThreads) {
-    const int s = s0 + threadIdx.x;
-    int any = 0, all = 1;
-    if (s < nslab) {
-      const int64_t r0 = (int64_t)s * 64;
-#pragma unroll 16
-      for (int e = 0; e < 64; ++e) {
-        const int64_t row = r0 + e;
-        const int v = row < N ? ids[row] : -1;
-        any |= v == a;
-        all &= v == a;
-      }
+    // a warp looks at 32 slabs, lane e keeps what slab e is
+    bool any = false, all = false;
+    const int w0 = s0 + warp * 32;
+#pragma unroll 8
+    for (int e = 0; e < 32; ++e) {
+      const int64_t row = (int64_t)(w0 + e) * 64 + lane;
+      const bool x = row < N && ids[row] == a, y = row + 32 < N && ids[row + 32] == a;
+      const unsigned vx = __ballot_sync(0xffffffffu, x), vy = __ballot_sync(0xffffffffu, y);
+      if (lane == e) { any = (vx | vy) != 0u; all = (vx & vy) == 0xffffffffu; }
     }
-    const unsigned vote = __ballot_sync(0xffffffffu, any != 0);
+    const unsigned vote = __ballot_sync(0xffffffffu, any);
     if (lane == 0) warp_cnt[warp] = __popc(vote);
     __syncthreads();
     int ahead = 0, sum = 0;
@@ -125,7 +143,7 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict_
       ahead += w < warp ? c : 0;
       sum += c;
     }
-    if (any) mine[at + ahead + __popc(vote & ((1u << lane) - 1u))] = (uint32_t)s | (all ? 0u : 0x80000000u);
+    if (any) mine[at + ahead + __popc(vote & ((1u << lane) - 1u))] = (uint32_t)(w0 + lane) | (all ? 0u : 0x80000000u);
     at += sum;
     __syncthreads();
   }
@@ -133,6 +151,31 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict_
 }
 
 // ------------------------------------------------------------------------------------------------ T of rows in mixed groups
+// The distinct adapters of the rows [row0, row0 + rows), rows 64 or 128, ascending, into ad (by lane 0); returns how many, kMaxAd + 1 if more than
+// kMaxAd.  Whole warp.
+constexpr int kMaxAd = 8;
+__device__ __forceinline__ int tile_adapters(const int* __restrict__ ids, int64_t N, int L, int64_t row0, int rows, int lane, int* ad) {
+  unsigned v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int64_t row = row0 + lane + 32 * e;
+    v[e] = lane + 32 * e < rows && row < N ? (unsigned)clean_id(ids[row], L) : 0xffffffffu;       // -1 is 0xffffffff: none
+  }
+  int n = 0;
+  unsigned last = 0;
+  while (true) {
+    unsigned low = 0xffffffffu;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if ((n == 0 || v[e] > last) && v[e] < low) low = v[e];
+    low = __reduce_min_sync(0xffffffffu, low);
+    if (low == 0xffffffffu) return n;
+    if (n == kMaxAd) return kMaxAd + 1;
+    if (ad && lane == 0) ad[n] = (int)low;
+    last = low;
+    ++n;
+  }
+}
+
 struct ProjParams {
   const bf16* In; int64_t N; int K;
   const bf16* F; int64_t strideF;           // f_mn 0: F_a is r x K, row-major; 1: K x r
@@ -140,12 +183,14 @@ struct ProjParams {
   const float* scale; const int* ids;
   float* T; bf16* P;                        // T: N x r; P: N x 3 rp
   int r, rp, L;
-  int all_rows;                             // every row goes this way
-  int unit;                                 // rows of a CTA, a divisor of 16
+  int want_T;                               // T (fp32) is wanted in every row, else in those of mixed groups
+  int all_rows;                             // every row goes by rows_kernel
+  int tile_rows;
+  int unit;                                 // rows of a CTA of rows_kernel, a divisor of tile_rows
   int first;                                // the call's first kernel
   int* status;
-  // project_kernel
-  int nk, tile_rows, ns, slot_bytes, in_bytes, f_bytes, q_max, tmem_cols;
+  // project_tc_kernel
+  int nk, csize, ns, slot_bytes, in_bytes, f_bytes, q_max, tmem_cols;
 };
 
 constexpr int kRowsThreads = 256;
@@ -158,8 +203,9 @@ __device__ __forceinline__ void put_T(const ProjParams& p, int64_t row, int k, f
   if (k < p.r) p.T[row * p.r + k] = v;
 }
 
-// A CTA has `unit` rows of one group and, where gridDim.y > 1, eight of the r values.  f_mn 0: a warp a value, lanes along K; f_mn 1:
-// a thread has eight neighbouring values and every so manieth row of F_a.
+// Rows of tiles with more adapters than project_tc_kernel takes (there: the rows of uniform groups), or all rows where they are few.  A CTA
+// has `unit` rows and, where gridDim.y > 1, eight of the r values.  f_mn 0: a warp a value, lanes along K; f_mn 1: a thread has eight
+// neighbouring values and every so manieth row of F_a.
 __global__ void __launch_bounds__(kRowsThreads)
 rows_kernel(const ProjParams p) {
   __shared__ float red[kRowsThreads / 32][32][8];
@@ -168,15 +214,14 @@ rows_kernel(const ProjParams p) {
   dep_launch();
   if (p.first && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = AB_OK;
   const int64_t row0 = (int64_t)blockIdx.x * p.unit;
-  bool work = p.all_rows != 0;
-  if (!work) {
-    const int64_t g0 = row0 & ~(int64_t)(kG - 1);
-    const int64_t row = g0 + (lane & 15);
-    const int v = row < p.N ? clean_id(p.ids[row], p.L) : -3, v0 = __shfl_sync(0xffffffffu, v, 0);
-    work = __any_sync(0xffffffffu, v != -3 && v != v0);
-  }
+  const bool work = p.all_rows || tile_adapters(p.ids, p.N, p.L, row0 / p.tile_rows * p.tile_rows, p.tile_rows, lane, nullptr) > kMaxAd;
   if (work) {
     for (int64_t row = row0; row < row0 + p.unit && row < p.N; ++row) {
+      if (!p.all_rows) {                       // a uniform group: not here
+        const int64_t other = (row & ~(int64_t)(kG - 1)) + (lane & (kG - 1));
+        const int v = other < p.N ? clean_id(p.ids[other], p.L) : -3, v0 = __shfl_sync(0xffffffffu, v, 0);
+        if (!__any_sync(0xffffffffu, v != -3 && v != v0)) continue;
+      }
       const int a = clean_id(p.ids[row], p.L);
       const float s = a < 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
       const uint4* x = reinterpret_cast<const uint4*>(p.In + row * (int64_t)p.K);
@@ -255,45 +300,66 @@ rows_kernel(const ProjParams p) {
   if (!p.first) dep_wait();          // this kernel is done only after the one before it
 }
 
-// ------------------------------------------------------------------------------------------------ T of uniform groups
+// ------------------------------------------------------------------------------------------------ clusters
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+// ------------------------------------------------------------------------------------------------ T by tiles
+// A cluster has a tile of rows and up to 128 of the r values (blockIdx.y), each of its CTAs a part of the reduction.  Every adapter that the
+// tile's rows have gets columns of its own in the accumulator, for all rows of the tile; a row takes its own adapter's.  Four slabs
+// (16 MMA steps) are summed in TMEM, the rest in registers: the tensor cores cut a sum off at every step (measured: 2e-8 of T a step),
+// registers round.  The parts meet in the shared memory of the CTA that finishes a share of the rows, in rank order.
+//
+// A slab costs a CTA about 500 cycles of issuing whatever its size, so several CTAs share an SM and long reductions are cut.
 constexpr int kProjTcThreads = 192;       // 0 = TMA producer, 1 = MMA issuer and TMEM owner, 2..5 = epilogue
 constexpr int kMaxStages = 8;
+constexpr int kFlush = 4;                 // slabs
 struct ProjBars {
-  uint64_t full[kMaxStages], empty[kMaxStages], done, drained;
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
   uint32_t tmem_base;
   int abort_any;
-  int nad, ad[8], group[8];               // the tile's adapters, and the adapter of each of its groups
+  int nad, whole, ad[kMaxAd];             // adapters of the tile; all of its rows are handled here
+  int row_ad[128];                        // a row's adapter, -1 none, -2: not handled here; + 0x40000000: T is wanted in fp32
 };
 
+template <int kChunks>                    // up to 16 kChunks values of r a CTA
 __global__ void __launch_bounds__(kProjTcThreads)
 project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmF, const ProjParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   ProjBars* b = reinterpret_cast<ProjBars*>(ring + (size_t)p.ns * p.slot_bytes);
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const int64_t row0 = (int64_t)blockIdx.x * p.tile_rows;
+  const int tile = (int)blockIdx.x / p.csize, rank = (int)blockIdx.x - tile * p.csize;
+  const int64_t row0 = (int64_t)tile * p.tile_rows;
+  const int kc0 = (int)blockIdx.y * 128, cols = p.rp - kc0 < 128 ? p.rp - kc0 : 128;
+  const int per = (p.nk + p.csize - 1) / p.csize, i0 = rank * per, i1 = i0 + per < p.nk ? i0 + per : p.nk;
   dep_launch();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
-    mbar_init(&b->done, 1);
-    mbar_init(&b->drained, 4);
+    for (int i = 0; i < 2; ++i) { mbar_init(&b->acc_full[i], 1); mbar_init(&b->acc_empty[i], 4); }
     b->abort_any = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tmIn); tma_prefetch_desc(&tmF);
   }
   if (warp == 0) {
-    bool bad;
-    const int g = group_ids(p.ids, p.N, p.L, row0, lane, bad);
-    const int ng = p.tile_rows / kG;
-    int nad = 0;
-    for (int i = 0; i < ng; ++i) {
-      const int v = __shfl_sync(0xffffffffu, g, i);
-      if (lane == 0) b->group[i] = v;
-      bool seen = v < 0;
-      for (int e = 0; e < i; ++e) seen |= __shfl_sync(0xffffffffu, g, e) == v;
-      if (!seen) { if (lane == 0) b->ad[nad] = v; ++nad; }
+    int n = tile_adapters(p.ids, p.N, p.L, row0, p.tile_rows, lane, b->ad);
+    const int whole = n <= kMaxAd;
+    if (!whole) {                          // the uniform groups alone
+      bool bad;
+      const int g = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+      n = 0;
+      const int ng = p.tile_rows / kG;
+      for (int i = 0; i < ng; ++i) {
+        const int v = __shfl_sync(0xffffffffu, g, i);
+        if (v >= 0 && !__any_sync(0xffffffffu, lane < i && g == v)) { if (lane == 0) b->ad[n] = v; ++n; }
+      }
     }
-    if (lane == 0) b->nad = nad;
+    if (lane == 0) { b->nad = n; b->whole = whole; }
   }
   if (warp == 1) tmem_alloc(&b->tmem_base, p.tmem_cols);
   tc_fence_before();
@@ -301,13 +367,15 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
   tc_fence_after();
   const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
   const int nad = (int)uniform(*reinterpret_cast<volatile int*>(&b->nad));
+  const int qw = warp & 3;                 // quarter of the TMEM lanes this warp may read = its 32 rows of the tile
+  float R[kChunks][16];
 
   if (warp == 0) {
     int slot = 0, ph = 1;
     bool ok = true;
     for (int q0 = 0; q0 < nad && ok; q0 += p.q_max) {
       const int q = nad - q0 < p.q_max ? nad - q0 : p.q_max;
-      for (int i = 0; i < p.nk; ++i) {
+      for (int i = i0; i < i1; ++i) {
         if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
         if (elect_one()) {
           uint8_t* dst = ring + (size_t)slot * p.slot_bytes;
@@ -317,8 +385,8 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
           for (int e = 0; e < q; ++e) {
             uint8_t* df = dst + p.in_bytes + e * p.f_bytes;
             const int a = b->ad[q0 + e];
-            if (p.f_mn) for (int h = 0; h * 8192 < p.f_bytes; ++h) tma_load_3d(df + h * 8192, &tmF, bar, 64 * h, i * 64, a);
-            else tma_load_3d(df, &tmF, bar, i * 64, 0, a);
+            if (p.f_mn) for (int h = 0; h * 8192 < p.f_bytes; ++h) tma_load_3d(df + h * 8192, &tmF, bar, kc0 + 64 * h, i * 64, a);
+            else tma_load_3d(df, &tmF, bar, i * 64, kc0, a);
           }
         }
         __syncwarp();
@@ -326,87 +394,133 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
       }
     }
   } else if (warp == 1) {
-    const uint32_t idesc = instr_desc_bf16(128, p.rp, 0, p.f_mn), base = uniform(smem_u32(ring));
+    const uint32_t idesc = instr_desc_bf16(128, cols, 0, p.f_mn), base = uniform(smem_u32(ring));
     const uint64_t dI = smem_desc_sw128(base, 16), dF = smem_desc_sw128(base + p.in_bytes, p.f_mn ? 8192 : 16);
     const uint64_t f_step = p.f_mn ? 128u : 2u, slot_step = (uint64_t)(p.slot_bytes >> 4), q_step = (uint64_t)(p.f_bytes >> 4);
-    int slot = 0, ph = 0, pass = 0;
+    int slot = 0, ph = 0, flush = 0;
     bool ok = true;
-    for (int q0 = 0; q0 < nad && ok; q0 += p.q_max, ++pass) {
+    for (int q0 = 0; q0 < nad && ok; q0 += p.q_max) {
       const int q = nad - q0 < p.q_max ? nad - q0 : p.q_max;
-      if (pass > 0) {
-        if (!mbar_wait_warp(&b->drained, (pass - 1) & 1)) { raise(&b->abort_any, p.status); break; }
-        tc_fence_after();
-      }
-      for (int i = 0; i < p.nk; ++i) {
+      for (int i = i0; i < i1; ++i) {
+        const int in = (i - i0) % kFlush, buf = flush & 1;
+        if (in == 0) {
+          if (!mbar_wait_warp(&b->acc_empty[buf], ((flush >> 1) & 1) ^ 1)) { raise(&b->abort_any, p.status); ok = false; break; }
+          tc_fence_after();
+        }
         if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
         tc_fence_after();
         const uint64_t da = dI + slot_step * slot, db = dF + slot_step * slot;
+        const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1));
         const int ksteps = (p.K - i * 64 + 15) >> 4;
+        const bool last = in == kFlush - 1 || i + 1 == i1;
         if (elect_one()) {
           for (int e = 0; e < q; ++e) {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-              if (kk < ksteps) tc_mma_bf16(tmem + e * p.rp, da + 2 * kk, db + q_step * e + f_step * kk, idesc, (i | kk) != 0);
+              if (kk < ksteps) tc_mma_bf16(tacc + e * cols, da + 2 * kk, db + q_step * e + f_step * kk, idesc, (in | kk) != 0);
           }
           tc_commit(&b->empty[slot]);
+          if (last) tc_commit(&b->acc_full[buf]);
         }
         __syncwarp();
+        if (last) ++flush;
         if (++slot == p.ns) { slot = 0; ph ^= 1; }
       }
-      if (ok && elect_one()) tc_commit(&b->done);
-      __syncwarp();
     }
   } else {
-    const int qw = warp & 3;                 // quarter of the TMEM lanes this warp may read = its 32 rows of the tile
     const int lrow = qw * 32 + lane;
     const int64_t row = row0 + lrow;
     const bool live = lrow < p.tile_rows && row < p.N;
-    const int a = live ? b->group[lrow / kG] : -2;
-    const float s = a < 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
-    if (a == -1) {                           // no adapter: zeros
-      for (int k = 0; k < p.r; k += 4) *reinterpret_cast<float4*>(p.T + row * p.r + k) = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int k = 0; k < 3 * p.rp; k += 8) *reinterpret_cast<uint4*>(p.P + row * 3 * p.rp + k) = make_uint4(0u, 0u, 0u, 0u);
+    const int a = live ? clean_id(p.ids[row], p.L) : -1;
+    {
+      const int g0 = (int)__shfl_sync(0xffffffffu, a, lane & 16);
+      const unsigned same = __ballot_sync(0xffffffffu, a == g0 || !live);
+      const bool mixed = ((same >> (lane & 16)) & 0xffffu) != 0xffffu;
+      b->row_ad[lrow] = !live || (mixed && !b->whole) ? -2 : p.want_T || mixed ? (a < 0 ? 0x7fffffff : a | 0x40000000) : a;
     }
-    int pass = 0;
-    for (int q0 = 0; q0 < nad; q0 += p.q_max, ++pass) {
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) R[c][i] = 0.f;
+    bool ok = true;
+    int flush = 0;
+    for (int q0 = 0; q0 < nad && ok; q0 += p.q_max) {
       const int q = nad - q0 < p.q_max ? nad - q0 : p.q_max;
-      if (!mbar_wait_warp(&b->done, pass & 1)) { raise(&b->abort_any, p.status); break; }
-      tc_fence_after();
-      for (int e = 0; e < q; ++e) {
-        const bool mine = a >= 0 && a == b->ad[q0 + e];
-        if (!__any_sync(0xffffffffu, mine)) continue;
-        for (int c = 0; c < p.rp; c += 16) {
-          float v[16];
-          tmem_ld16(tmem + ((uint32_t)(qw * 32) << 16) + e * p.rp + c, v);
-          if (!mine) continue;
-          uint32_t h[8], m[8], l[8];
+      for (int i = i0; i < i1 && ok; i += kFlush, ++flush) {
+        const int buf = flush & 1;
+        ok = mbar_wait_warp(&b->acc_full[buf], (flush >> 1) & 1);
+        if (!ok) { raise(&b->abort_any, p.status); break; }
+        tc_fence_after();
+        const uint32_t t = tmem + (uint32_t)(buf * (p.tmem_cols >> 1)) + ((uint32_t)(qw * 32) << 16);
+        for (int e = 0; e < q; ++e) {
+          const bool take = a >= 0 && a == b->ad[q0 + e];
+          if (!__any_sync(0xffffffffu, take)) continue;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            bf16 hh[2], mm[2], ll[2];
-            v[2 * i] *= s; v[2 * i + 1] *= s;
-            cut(v[2 * i], hh[0], mm[0], ll[0]);
-            cut(v[2 * i + 1], hh[1], mm[1], ll[1]);
-            h[i] = (uint32_t)__bfloat16_as_ushort(hh[0]) | ((uint32_t)__bfloat16_as_ushort(hh[1]) << 16);
-            m[i] = (uint32_t)__bfloat16_as_ushort(mm[0]) | ((uint32_t)__bfloat16_as_ushort(mm[1]) << 16);
-            l[i] = (uint32_t)__bfloat16_as_ushort(ll[0]) | ((uint32_t)__bfloat16_as_ushort(ll[1]) << 16);
-          }
-          bf16* P = p.P + row * 3 * p.rp + c;
+          for (int c = 0; c < kChunks; ++c) {
+            if (16 * c >= cols) continue;
+            float v[16];
+            tmem_ld16(t + e * cols + 16 * c, v);
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            *reinterpret_cast<uint4*>(P + 8 * g) = make_uint4(h[4 * g], h[4 * g + 1], h[4 * g + 2], h[4 * g + 3]);
-            *reinterpret_cast<uint4*>(P + p.rp + 8 * g) = make_uint4(m[4 * g], m[4 * g + 1], m[4 * g + 2], m[4 * g + 3]);
-            *reinterpret_cast<uint4*>(P + 2 * p.rp + 8 * g) = make_uint4(l[4 * g], l[4 * g + 1], l[4 * g + 2], l[4 * g + 3]);
-            if (c + 8 * g < p.r) {
-              float4* t = reinterpret_cast<float4*>(p.T + row * p.r + c + 8 * g);
-              t[0] = make_float4(v[8 * g], v[8 * g + 1], v[8 * g + 2], v[8 * g + 3]);
-              t[1] = make_float4(v[8 * g + 4], v[8 * g + 5], v[8 * g + 6], v[8 * g + 7]);
-            }
+            for (int k = 0; k < 16; ++k) R[c][k] += take ? v[k] : 0.f;
           }
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b->acc_empty[buf]);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&b->drained);
+    }
+  }
+
+  // The ring has been read: it takes the parts, [rank][row of the share][cols], rows 16 bytes apart more than they are long
+  const int share = p.tile_rows / p.csize, pitch = cols + 4;
+  float* red = reinterpret_cast<float*>(ring);
+  if (p.csize > 1) { cluster_arrive(); cluster_wait(); }       // every CTA of the cluster runs, and is through with its ring
+  if (warp >= 2) {
+    const int lrow = qw * 32 + lane;
+    if (lrow < p.tile_rows) {
+      const int owner = lrow / share, at = (rank * share + lrow - owner * share) * pitch;
+      const uint32_t to = p.csize > 1 ? cluster_addr(smem_u32(red + at), (uint32_t)owner) : 0u;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        if (16 * c >= cols) continue;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          if (p.csize > 1)
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(16 * c + i) * 4), "f"(R[c][i]), "f"(R[c][i + 1]),
+                         "f"(R[c][i + 2]), "f"(R[c][i + 3])
+                         : "memory");
+          else
+            *reinterpret_cast<float4*>(red + at + 16 * c + i) = make_float4(R[c][i], R[c][i + 1], R[c][i + 2], R[c][i + 3]);
+        }
+      }
+    }
+  }
+  if (p.csize > 1) { cluster_arrive(); cluster_wait(); }
+  if (warp >= 2) {
+    if (p.csize == 1) named_bar_sync(1, 128);
+    const int oct = cols / 8;
+    for (int u = threadIdx.x - 64; u < share * oct; u += 128) {
+      const int lr = u / oct, k = (u - lr * oct) * 8, code = b->row_ad[rank * share + lr];
+      if (code == -2) continue;
+      const int64_t row = row0 + rank * share + lr;
+      const int a = code == 0x7fffffff ? -1 : code < 0 ? -1 : code & 0x3fffffff;
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (a >= 0) {
+        for (int q = 0; q < p.csize; ++q) {
+          const float4* f = reinterpret_cast<const float4*>(red + (q * share + lr) * pitch + k);
+          const float4 x = f[0], y = f[1];
+          v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+        }
+        const float s = p.scale ? p.scale[a] : 1.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= s;
+      }
+      put_pieces(p.P + row * 3 * p.rp + kc0 + k, p.rp, v);
+      if (code >= 0x40000000 && kc0 + k < p.r) {
+        float4* t = reinterpret_cast<float4*>(p.T + row * p.r + kc0 + k);
+        t[0] = make_float4(v[0], v[1], v[2], v[3]);
+        t[1] = make_float4(v[4], v[5], v[6], v[7]);
+      }
     }
     fence_proxy_async_all();
   }
@@ -439,24 +553,101 @@ struct OutParams {
   int* status;
 };
 
-// sum_k G_a(f, k) T[k] of one row and one output feature
-__device__ __forceinline__ float small_dot(const OutParams& p, int a, int f, const float* __restrict__ T) {
-  const bf16* g = p.G + a * p.strideG;
-  float v = 0.f;
+// v[e] += sum_k G_a(f, k) T[row][k] for 16 rows from row0 (those below `end`), each with its own adapter; lane = output feature f.  T by way
+// of a piece of shared memory of the warp (16 x 64 floats), 64 values at a time.  Every sum is formed for every row that shares a loop
+// and chosen afterwards, not multiplied by zero: straight code, whose many independent sums hide each other's latency.
+__device__ __forceinline__ void load_g(const OutParams& p, const bf16* __restrict__ g, int f, int k0, uint4 (&u)[2]) {
+  // 16 values from k0, or 8 where r ends there
   if (!p.mn) {
-    const uint4* q = reinterpret_cast<const uint4*>(g + (int64_t)f * p.r);
-#pragma unroll 2
-    for (int k = 0; k < p.r / 8; ++k) {
-      const uint4 u = q[k];
-      const float4 t0 = *reinterpret_cast<const float4*>(T + 8 * k), t1 = *reinterpret_cast<const float4*>(T + 8 * k + 4);
-      const float t[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
-      dot8(u, t, v);
-    }
+    const uint4* q = reinterpret_cast<const uint4*>(g + (int64_t)f * p.r + k0);
+    u[0] = q[0];
+    u[1] = k0 + 8 < p.r ? q[1] : make_uint4(0u, 0u, 0u, 0u);
   } else {
-#pragma unroll 8
-    for (int k = 0; k < p.r; ++k) v = fmaf(__bfloat162float(g[(int64_t)k * p.P + f]), T[k], v);
+    const unsigned short* q = reinterpret_cast<const unsigned short*>(g) + (int64_t)k0 * p.P + f;
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool in = k0 + 2 * e < p.r;
+      const uint32_t lo = in ? q[(int64_t)(2 * e) * p.P] : 0u, hi = in ? q[(int64_t)(2 * e + 1) * p.P] : 0u;
+      w[e] = lo | (hi << 16);
+    }
+    u[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    u[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
-  return v;
+}
+__device__ __forceinline__ float sum16(const uint4 (&u)[2], const float* t) {
+  const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
+  float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float4 x = *reinterpret_cast<const float4*>(t + 4 * e);
+    s0 = fmaf(__uint_as_float(w[2 * e] << 16), x.x, s0);
+    s1 = fmaf(__uint_as_float(w[2 * e] & 0xffff0000u), x.y, s1);
+    s0 = fmaf(__uint_as_float(w[2 * e + 1] << 16), x.z, s0);
+    s1 = fmaf(__uint_as_float(w[2 * e + 1] & 0xffff0000u), x.w, s1);
+  }
+  return s0 + s1;
+}
+__device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int64_t end, int f, int lane, float* Ts, float (&v)[kG]) {
+  const int ff = f < p.P ? f : p.P - 1;       // a lane past the last feature reads what its neighbour reads
+  const int rows = (int)(end - row0 < kG ? end - row0 : kG);
+  const int id = lane < rows ? clean_id(p.ids[row0 + lane], p.L) : -1;
+  const int before = __shfl_up_sync(0xffffffffu, id, 1);
+  const unsigned heads = __ballot_sync(0xffffffffu, id >= 0 && (lane == 0 || id != before));      // first rows of runs
+  const unsigned live = __ballot_sync(0xffffffffu, id >= 0);
+  const int runs = __popc(heads);
+  if (runs == 0) return;
+  for (int k0 = 0; k0 < p.r; k0 += 64) {
+    const int kn = p.r - k0 < 64 ? p.r - k0 : 64;
+    __syncwarp();
+    // a row in two lanes' hands; what r does not fill of the last 16 values is 0
+    {
+      const int e = lane >> 1;
+      for (int c = (lane & 1) * 4; c < ((kn + 15) & ~15); c += 8)
+        *reinterpret_cast<float4*>(Ts + e * 64 + c) =
+            e < rows && c < kn ? *reinterpret_cast<const float4*>(p.T + (row0 + e) * p.r + k0 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __syncwarp();
+    if (runs <= 2) {                           // the end of one run and the beginning of the next
+      const int h0 = __ffs(heads) - 1, h1 = runs > 1 ? 31 - __clz(heads) : kG;
+      const bf16* ga = p.G + __shfl_sync(0xffffffffu, id, h0) * p.strideG;
+      const bf16* gb = p.G + __shfl_sync(0xffffffffu, id, h1 < kG ? h1 : h0) * p.strideG;
+      const unsigned first = live & ((1u << h1) - 1u), second = live & ~((1u << h1) - 1u);
+      uint4 ua[2], ub[2];
+      load_g(p, ga, ff, k0, ua);
+      load_g(p, gb, ff, k0, ub);
+      for (int k1 = 0; k1 < kn; k1 += 16) {
+        uint4 na[2], nb[2];
+        const int kx = k1 + 16 < kn ? k0 + k1 + 16 : k0;
+        load_g(p, ga, ff, kx, na);
+        load_g(p, gb, ff, kx, nb);
+#pragma unroll
+        for (int e = 0; e < kG; ++e) {
+          const float x = sum16(ua, Ts + e * 64 + k1), y = sum16(ub, Ts + e * 64 + k1);
+          v[e] += ((first >> e) & 1u) ? x : ((second >> e) & 1u) ? y : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) { ua[i] = na[i]; ub[i] = nb[i]; }
+      }
+    } else {                                   // an adapter a row, eight rows at a time
+      for (int k1 = 0; k1 < kn; k1 += 16) {
+#pragma unroll
+        for (int h = 0; h < kG; h += 8) {
+          uint4 u[8][2];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int a = __shfl_sync(0xffffffffu, id, h + e);
+            load_g(p, p.G + (a >= 0 ? a : 0) * p.strideG, ff, k0 + k1, u[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float x = sum16(u[e], Ts + (h + e) * 64 + k1);
+            v[h + e] += ((live >> (h + e)) & 1u) ? x : 0.f;
+          }
+        }
+      }
+    }
+  }
 }
 
 constexpr int kWideThreads = 192;
@@ -491,7 +682,8 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* stg = ring + (size_t)p.ns * p.slot_bytes;              // per epilogue warp two tiles of 32 rows x 32 features
-  WideBars* b = reinterpret_cast<WideBars*>(stg + 4 * 2 * 2048);
+  float* tbuf = reinterpret_cast<float*>(stg + 4 * 2 * 2048);     // and T of 16 rows
+  WideBars* b = reinterpret_cast<WideBars*>(tbuf + 4 * kG * 64);
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   dep_launch();
   if (threadIdx.x == 0) {
@@ -614,36 +806,63 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1)) + lane_base;
       const bool live = f0 < p.P;
       for (int g0 = 0; g0 < ngroups; g0 += 2) {
+        if (!live || (int64_t)row0 + g0 * kG >= p.N) {
+          if (g0 + 2 >= ngroups) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&b->acc_empty[buf]);
+          }
+          continue;
+        }
+        uint8_t* tile_s = my + (nst & 1) * 2048;
+        ++nst;
+        if (lane == 0) tma_store_wait_read<1>();
+        __syncwarp();
+        const bool simt = ((mixed >> g0) & 3u) != 0u;
         uint32_t v[2][16];
-        tmem_ld16_nowait(tacc + g0 * kG, v[0]);
-        if (g0 + 1 < ngroups) tmem_ld16_nowait(tacc + g0 * kG + kG, v[1]);
+        if (!simt) {                     // features 0..15 and 16..31 of the warp, 32 rows
+          tmem_ld_16x32_nowait(tacc + g0 * kG, v[0]);
+          tmem_ld_16x32_nowait(tacc + (16u << 16) + g0 * kG, v[1]);
+        } else {                         // a feature a lane, 16 + 16 rows
+          tmem_ld16_nowait(tacc + g0 * kG, v[0]);
+          tmem_ld16_nowait(tacc + g0 * kG + kG, v[1]);
+        }
         tmem_wait_ld();
         if (g0 + 2 >= ngroups) {         // the last columns are in registers: hand the accumulator back
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&b->acc_empty[buf]);
         }
-        if (!live || (int64_t)row0 + g0 * kG >= p.N) continue;
+        if (!simt) {
+          // eight rows (columns 8 j ..) of 32 features are four fragments; transposed they are 8 rows of 64 bytes, whose 16-byte pieces
+          // lie where the swizzle puts them
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!((mixed >> (g0 + h)) & 1u)) continue;
-          const int f = f0 + lane;
+          for (int j = 0; j < 4; ++j) {
+            uint32_t w[4];
 #pragma unroll
-          for (int e = 0; e < kG; ++e) {
-            const int64_t row = (int64_t)row0 + (g0 + h) * kG + e;
-            const int a = row < p.N ? clean_id(p.ids[row], p.L) : -1;
-            if (a >= 0 && f < p.P) v[h][e] = __float_as_uint(__uint_as_float(v[h][e]) + small_dot(p, a, f, p.T + row * p.r));
+            for (int h = 0; h < 4; ++h) {
+              const __nv_bfloat162 x = __floats2bfloat162_rn(__uint_as_float(v[h >> 1][4 * j + 2 * (h & 1)]),
+                                                             __uint_as_float(v[h >> 1][4 * j + 2 * (h & 1) + 1]));
+              w[h] = *reinterpret_cast<const uint32_t*>(&x);
+            }
+            const int r = 8 * j + (lane & 7), piece = (lane >> 3) ^ ((r >> 1) & 3);
+            stmatrix_x4_trans(smem_u32(tile_s) + r * 64 + piece * 16, w[0], w[1], w[2], w[3]);
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float d[kG];
+#pragma unroll
+            for (int e = 0; e < kG; ++e) d[e] = __uint_as_float(v[h][e]);
+            if ((mixed >> (g0 + h)) & 1u)
+              add_mixed(p, (int64_t)row0 + (g0 + h) * kG, p.N, f0 + lane, lane, tbuf + (warp - 2) * kG * 64, d);
+#pragma unroll
+            for (int e = 0; e < kG; ++e) {
+              const int r = h * kG + e;
+              *reinterpret_cast<bf16*>(tile_s + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2) = __float2bfloat16_rn(d[e]);
+            }
           }
         }
-        uint8_t* tile_s = my + (nst & 1) * 2048;
-        ++nst;
-        if (lane == 0) tma_store_wait_read<1>();
-        __syncwarp();
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < kG; ++e)
-            *reinterpret_cast<bf16*>(tile_s + (h * kG + e) * 64 + lane * 2) = __float2bfloat16_rn(__uint_as_float(v[h][e]));
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
@@ -678,14 +897,6 @@ struct FewBars {
   uint32_t tmem_base;
   int abort_any;
 };
-__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-
 constexpr int kFewRows = 128;
 __global__ void __launch_bounds__(kWideThreads, 1)
 few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const OutParams p) {
@@ -693,7 +904,8 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const int share = (p.bn + p.csize - 1) / p.csize;               // rows that a CTA finishes
   float* red = reinterpret_cast<float*>(ring + (size_t)p.ns * p.slot_bytes);      // [csize][share][128]
-  FewBars* b = reinterpret_cast<FewBars*>(red + (size_t)p.csize * share * 128);
+  float* tbuf = red + (size_t)p.csize * share * 128;              // T of 16 rows for each epilogue warp
+  FewBars* b = reinterpret_cast<FewBars*>(tbuf + 4 * kG * 64);
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int ft = (int)blockIdx.x / p.csize, rank = (int)blockIdx.x - ft * p.csize, f0 = ft * 128;
   const int per = (p.nk + p.csize - 1) / p.csize, i0 = rank * per, i1 = i0 + per < p.nk ? i0 + per : p.nk;
@@ -751,6 +963,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
     __syncwarp();
   }
   const int qw = warp & 3, f = f0 + qw * 32 + lane, t0 = rank * share;
+  const int t1 = t0 + share < p.N ? t0 + share : (int)p.N;        // the rows that this CTA finishes
   bool ok = true;
   if (warp >= 2) {
     dep_wait();                            // T is complete
@@ -760,11 +973,8 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
       if (__any_sync(0xffffffffu, bad) && lane == 0) atomicExch(p.status, (int)AB_ERR_INVALID_ARG);
     }
 #pragma unroll
-    for (int e = 0; e < kG; ++e) {
-      const int t = t0 + e;
-      const int a = e < share && t < p.N ? clean_id(p.ids[t], p.L) : -1;
-      acc[e] = a >= 0 && f < p.P ? small_dot(p, a, f, p.T + (int64_t)t * p.r) : 0.f;
-    }
+    for (int e = 0; e < kG; ++e) acc[e] = 0.f;
+    if (t0 < t1 && f0 + qw * 32 < p.P) add_mixed(p, t0, t1, f, lane, tbuf + (warp - 2) * kG * 64, acc);
     ok = mbar_wait_warp(&b->acc_full, 0);
     if (!ok) raise(&b->abort_any, p.status);
   }
@@ -790,20 +1000,19 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
   }
   cluster_arrive();
   cluster_wait();                          // and has written its sums
-  if (warp >= 2 && f < p.P) {
-    for (int e0 = 0; e0 < share; e0 += kG) {
+  if (warp >= 2 && f0 + qw * 32 < p.P) {
+    for (int e0 = 0; t0 + e0 < t1; e0 += kG) {
+      if (e0 > 0) {
+#pragma unroll
+        for (int e = 0; e < kG; ++e) acc[e] = 0.f;
+        add_mixed(p, t0 + e0, t1, f, lane, tbuf + (warp - 2) * kG * 64, acc);
+      }
 #pragma unroll
       for (int e = 0; e < kG; ++e) {
-        const int t = t0 + e0 + e;
-        if (e0 + e >= share || t >= p.N) continue;
+        if (t0 + e0 + e >= t1 || f >= p.P) continue;
         float v = 0.f;
         for (int q = 0; q < p.csize; ++q) v += red[(q * share + e0 + e) * 128 + qw * 32 + lane];
-        float d = acc[e];
-        if (e0 > 0) {
-          const int a = clean_id(p.ids[t], p.L);
-          d = a >= 0 ? small_dot(p, a, f, p.T + (int64_t)t * p.r) : 0.f;
-        }
-        p.Out[(int64_t)t * p.P + f] = __float2bfloat16_rn(v + d);
+        p.Out[(int64_t)(t0 + e0 + e) * p.P + f] = __float2bfloat16_rn(v + acc[e]);
       }
     }
   }
@@ -828,21 +1037,20 @@ struct GradParams {
   int slices;
   int stacked;                              // the three pieces side by side as columns of one MMA
   int nb;                                   // 64-column boxes of the small operand a slab
-  int ns, slot_bytes, tmem_cols;
+  int ns, slot_bytes, bufs, tmem_cols;      // bufs: accumulators used in turn
   const int* ids; const uint32_t* list; const int* count;
   int check;                                // report bad map entries (no other kernel of the call does)
   int* status;
 };
-constexpr int kFlush = 8;                 // slabs (512 rows) a TMEM accumulator takes before it is added to fp32 registers: the tensor
-                                          // cores cut off what does not fit a sum, registers round
 struct GradBars {
   uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
   uint32_t tmem_base;
   int abort_any;
 };
 
+// Four slabs (256 rows) are summed in TMEM, the rest in registers, as in project_tc_kernel.
 template <int kChunks>                    // up to 16 kChunks values of r a CTA
-__global__ void __launch_bounds__(kWideThreads, 1)
+__global__ void __launch_bounds__(kWideThreads)
 adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_constant__ CUtensorMap tmS0,
                        const __grid_constant__ CUtensorMap tmAct1, const __grid_constant__ CUtensorMap tmS1, const GradParams p) {
   extern __shared__ uint8_t smem_raw[];
@@ -912,10 +1120,10 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
     bool ok = true;
     for (int e = e0, n = 0; e < e1 && ok; ++e, ++n) {
       const uint32_t entry = uniform(list[e]);
-      const int flush = n / kFlush, buf = flush & 1, in = n % kFlush;
+      const int flush = n / kFlush, buf = p.bufs > 1 ? flush & 1 : 0, in = n % kFlush, turn = p.bufs > 1 ? flush >> 1 : flush;
       const bool others = entry >> 31;
       if (in == 0) {
-        if (!mbar_wait_warp(&b->acc_empty[buf], ((flush >> 1) & 1) ^ 1)) { raise(&b->abort_any, p.status); break; }
+        if (!mbar_wait_warp(&b->acc_empty[buf], (turn & 1) ^ 1)) { raise(&b->abort_any, p.status); break; }
         tc_fence_after();
       }
       const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1));
@@ -961,8 +1169,8 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
     const int flushes = (e1 - e0 + kFlush - 1) / kFlush;
     bool ok = true;
     for (int n = 0; n < flushes && ok; ++n) {
-      const int buf = n & 1;
-      ok = mbar_wait_warp(&b->acc_full[buf], (n >> 1) & 1);
+      const int buf = p.bufs > 1 ? n & 1 : 0, turn = p.bufs > 1 ? n >> 1 : n;
+      ok = mbar_wait_warp(&b->acc_full[buf], turn & 1);
       if (!ok) { raise(&b->abort_any, p.status); break; }
       tc_fence_after();
       const uint32_t t = tmem + (uint32_t)(buf * (p.tmem_cols >> 1)) + lane_base;
@@ -1027,37 +1235,56 @@ int stack_map(CUtensorMap* m, const AdapterCall& c, const void* F, int rows, int
 }
 
 // T = s F In of all rows (two launches, or one for few rows); `first`: nothing of the call was launched before
-int launch_project(const AdapterCall& c, const void* In, int K, const void* F, int64_t strideF, bool f_mn, float* T, bf16* P, bool first, int* status) {
+int launch_project(const AdapterCall& c, const void* In, int K, const void* F, int64_t strideF, bool f_mn, float* T, bool want_T, bf16* P, bool first,
+                   int* status) {
+  const int sms = sm_count();
+  if (sms <= 0) return AB_ERR_CUDA;
   ProjParams p;
   std::memset(&p, 0, sizeof(p));
   const int rp = pad16(c.r);
   p.In = static_cast<const bf16*>(In); p.N = c.N; p.K = K; p.F = static_cast<const bf16*>(F); p.strideF = strideF; p.f_mn = f_mn ? 1 : 0;
   p.scale = c.scale; p.ids = c.ids; p.T = T; p.P = P; p.r = c.r; p.rp = rp; p.L = c.L; p.first = first ? 1 : 0; p.status = status;
+  p.want_T = want_T || c.N <= kFewRows ? 1 : 0;
   p.all_rows = c.N <= 64 ? 1 : 0;
-  p.unit = c.N <= 1024 ? 1 : c.N <= 8192 ? 4 : 16;
+  p.tile_rows = c.N > 1024 ? 128 : 64;
+  const int64_t tiles = (c.N + p.tile_rows - 1) / p.tile_rows;
+  // about 600 CTAs for the rows that go one by one
+  p.unit = 1;
+  while (p.unit < p.tile_rows && tiles * p.tile_rows / p.unit > 600) p.unit *= 2;
   const int64_t units = (c.N + p.unit - 1) / p.unit;
   const int ky = !f_mn && units <= 256 ? (rp + 7) / 8 : 1;
   AB_TRY(launch_after(rows_kernel, dim3((unsigned)units, (unsigned)ky), (unsigned)kRowsThreads, 0, 1, c.st, p));
   if (p.all_rows) return AB_OK;
+  const int cols = rp < 128 ? rp : 128;
   p.nk = (K + 63) / 64;
-  p.tile_rows = c.N > (int64_t)64 * 2 * sm_count() ? 128 : 64;
   p.in_bytes = p.tile_rows * 128;
-  p.f_bytes = f_mn ? (c.r + 63) / 64 * 8192 : rp * 128;
+  p.f_bytes = f_mn ? (cols + 63) / 64 * 8192 : cols * 128;
   const int room = p.f_bytes > 8192 ? p.f_bytes : 8192;
-  p.q_max = room / p.f_bytes < 512 / rp ? room / p.f_bytes : 512 / rp;
-  if (p.q_max > 8) p.q_max = 8;
+  p.q_max = room / p.f_bytes < 128 / cols ? room / p.f_bytes : 128 / cols;       // two accumulators in half of the columns: two CTAs an SM
+  if (p.q_max > kMaxAd) p.q_max = kMaxAd;
   p.slot_bytes = p.in_bytes + room;
   if (p.slot_bytes < 16384) p.slot_bytes = 16384;          // an MMA reads 128 rows of In, loaded or not
-  p.ns = 100 * 1024 / p.slot_bytes < kMaxStages ? 100 * 1024 / p.slot_bytes : kMaxStages;
-  if (p.ns < 3) p.ns = 3;
-  p.tmem_cols = pow2_cols(p.q_max * rp);
+  // three CTAs an SM; the ring takes the parts at the end
+  const int parts = p.tile_rows * (cols + 4) * 4;
+  p.ns = 72 * 1024 / p.slot_bytes < 3 ? 3 : 72 * 1024 / p.slot_bytes;
+  if (p.ns * p.slot_bytes < parts) p.ns = (parts + p.slot_bytes - 1) / p.slot_bytes;
+  p.csize = 8;
+  while (p.csize > 1 && (tiles * p.csize > 2 * sms || 2 * p.csize > p.nk)) p.csize >>= 1;
+  p.tmem_cols = 2 * pow2_cols(p.q_max * cols);
   CUtensorMap tmIn, tmF;
   AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.tile_rows));
-  AB_TRY(stack_map(&tmF, c, F, f_mn ? K : c.r, f_mn ? c.r : K, strideF, f_mn ? 64 : rp));
+  AB_TRY(stack_map(&tmF, c, F, f_mn ? K : c.r, f_mn ? c.r : K, strideF, f_mn ? 64 : cols));
   const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + sizeof(ProjBars);
-  AB_CUDA_OK(allow_smem(project_tc_kernel));
-  return launch_after(project_tc_kernel, (unsigned)((c.N + p.tile_rows - 1) / p.tile_rows), (unsigned)kProjTcThreads, smem, 1, c.st, tmIn, tmF, p);
+  const dim3 grid((unsigned)(tiles * p.csize), (unsigned)((rp + 127) / 128));
+  if (cols <= 64) {
+    AB_CUDA_OK(allow_smem(project_tc_kernel<4>));
+    return launch_after(project_tc_kernel<4>, grid, (unsigned)kProjTcThreads, smem, p.csize, c.st, tmIn, tmF, p);
+  }
+  AB_CUDA_OK(allow_smem(project_tc_kernel<8>));
+  return launch_after(project_tc_kernel<8>, grid, (unsigned)kProjTcThreads, smem, p.csize, c.st, tmIn, tmF, p);
 }
+
+constexpr int kTbuf = 4 * kG * 64 * 4;
 
 // Out = In W^T + T G^T; mn as in OutParams
 int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void* G, int64_t strideG, void* Out, int P, const float* T, const bf16* Tp,
@@ -1080,12 +1307,12 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
     p.slot_bytes = kABytes + p.bn * 128;
     const int share = (p.bn + p.csize - 1) / p.csize;
     const size_t red = (size_t)p.csize * share * 512;
-    p.ns = (int)((kMaxSmem - 2048 - red - sizeof(FewBars)) / p.slot_bytes);
+    p.ns = (int)((kMaxSmem - 2048 - red - kTbuf - sizeof(FewBars)) / p.slot_bytes);
     if (p.ns > kMaxStages) p.ns = kMaxStages;
     p.tmem_cols = pow2_cols(p.bn);
     AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn));
     AB_CUDA_OK(allow_smem(few_kernel));
-    return launch_after(few_kernel, (unsigned)(p.nft * p.csize), (unsigned)kWideThreads, 1024 + (size_t)p.ns * p.slot_bytes + red + sizeof(FewBars),
+    return launch_after(few_kernel, (unsigned)(p.nft * p.csize), (unsigned)kWideThreads, 1024 + (size_t)p.ns * p.slot_bytes + red + kTbuf + sizeof(FewBars),
                         p.csize, c.st, tmW, tmIn, p);
   }
   // rows of a tile: cycles of the busiest SM, a slab's operands arriving at 64 bytes a cycle or its MMAs, whichever is longer
@@ -1105,9 +1332,9 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
   AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn));
   AB_TRY(make_tensor_map_2d(&tmT, Tp, false, (uint64_t)c.N, 3 * rp, 3 * rp, 64, p.bn));
   AB_TRY(stack_map(&tmG, c, G, mn ? c.r : P, mn ? P : c.r, strideG, mn ? 64 : 128));
-  AB_TRY(make_tensor_map_plain(&tmOut, Out, (uint64_t)c.N, P, 32, 32));
+  AB_TRY(make_tensor_map_sw64(&tmOut, Out, (uint64_t)c.N, P, 32, 32));
   AB_CUDA_OK(allow_smem(wide_kernel));
-  const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + 4 * 2 * 2048 + sizeof(WideBars);
+  const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + 4 * 2 * 2048 + kTbuf + sizeof(WideBars);
   return launch_after(wide_kernel, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideThreads, smem, 1, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
 }
 
@@ -1151,8 +1378,10 @@ int launch_grads(const AdapterCall& c, const void* dY, float* dA, float* dB, con
   p.stacked = 3 * rp <= 256 ? 1 : 0;
   p.nb = p.stacked ? (3 * rp + 63) / 64 : ((rp < 128 ? rp : 128) + 63) / 64;
   p.slot_bytes = kABytes + p.nb * 8192;
-  p.ns = 200 * 1024 / p.slot_bytes < kMaxStages ? 200 * 1024 / p.slot_bytes : kMaxStages;
-  p.tmem_cols = 2 * pow2_cols(p.stacked ? 3 * rp : rp < 128 ? rp : 128);
+  const int acc = pow2_cols(p.stacked ? 3 * rp : rp < 128 ? rp : 128);
+  p.bufs = acc <= 128 ? 2 : 1;               // half of the columns: two CTAs an SM
+  p.tmem_cols = p.bufs * acc;
+  p.ns = 108 * 1024 / p.slot_bytes < kMaxStages ? 108 * 1024 / p.slot_bytes : kMaxStages;
   CUtensorMap act[2], small[2];
   int nj = 0;
   if (dA) {
@@ -1189,7 +1418,7 @@ int launch_grads(const AdapterCall& c, const void* dY, float* dA, float* dB, con
 }  // namespace
 
 bool adapter_tc_shape_ok(int64_t N, int m, int n, int r, int L, int dt) {
-  return dt == AB_BF16 && m % 8 == 0 && n % 8 == 0 && r % 8 == 0 && r <= 256 && N <= ((int64_t)1 << 30);
+  return dt == AB_BF16 && m % 8 == 0 && n % 8 == 0 && r % 8 == 0 && r <= 256 && N <= ((int64_t)1 << 30) && L < (1 << 30);
 }
 
 bool adapter_tc_supported(const AdapterCall& c, const void* dY, const void* out, const float* T, const float* dA, const float* dB) {
@@ -1204,7 +1433,7 @@ size_t adapter_tc_ws(int64_t N, int m, int n, int r, int L) { return tc_ws(nullp
 int adapter_tc_forward(const AdapterCall& c, void* y, float* T_save, void* ws) {
   const TcWs w = tc_ws(ws, c.N, c.m, c.n, c.r, c.L);
   float* T = T_save ? T_save : w.T;
-  AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, T, w.TP, true, w.status));
+  AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, T, T_save != nullptr, w.TP, true, w.status));
   return launch_out(c, c.x, c.n, false, c.A, c.strideA, y, c.m, T, w.TP, w.status);
 }
 
@@ -1213,17 +1442,17 @@ int adapter_tc_backward(const AdapterCall& c, const void* dY, const float* T_sav
   bool first = true;
   if (dA || dB) {
     const int64_t rows = dA && T_saved ? c.N : 0;
-    int64_t blocks = (rows * pad16(c.r) + kPrepThreads * 4 - 1) / (kPrepThreads * 4);
+    int64_t blocks = (rows * (pad16(c.r) / 8) + kPrepThreads - 1) / kPrepThreads;
     if (blocks > 1024) blocks = 1024;
     AB_TRY(launch_after(prep_kernel, (unsigned)(c.L + blocks), (unsigned)kPrepThreads, 0, 1, c.st, c.ids, c.N, c.L, w.list, w.count, w.nslab, T_saved, w.TP,
                         c.r, pad16(c.r), w.status));
     first = false;
   }
   if (dX || dB) {
-    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, w.UP, first, w.status));
+    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, false, w.UP, first, w.status));
     first = false;
   }
-  if (dA && !T_saved) AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, w.TP, first, w.status));
+  if (dA && !T_saved) AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, false, w.TP, first, w.status));
   if (dX) AB_TRY(launch_out(c, dY, c.m, true, c.B, c.strideB, dX, c.n, w.U, w.UP, w.status));
   if (dA || dB) AB_TRY(launch_grads(c, dY, dA, dB, w, !dX));
   return AB_OK;

@@ -1279,7 +1279,7 @@ int make_tensor_map_stack(CUtensorMap* m, const void* ptr, uint64_t count, uint6
   return rc == CUDA_SUCCESS ? AB_OK : AB_ERR_CUDA;
 }
 
-int make_tensor_map_plain(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
+int make_tensor_map_sw64(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return AB_ERR_CUDA;
   cuuint64_t dims[2] = {cols, rows};
@@ -1287,7 +1287,7 @@ int make_tensor_map_plain(CUtensorMap* m, const void* ptr, uint64_t rows, uint64
   cuuint32_t box[2] = {box_cols, box_rows};
   cuuint32_t estr[2] = {1, 1};
   CUresult rc = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return rc == CUDA_SUCCESS ? AB_OK : AB_ERR_CUDA;
 }

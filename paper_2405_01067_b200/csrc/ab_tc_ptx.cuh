@@ -179,6 +179,22 @@ __device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t (&r)[1
       : "r"(taddr)
       : "memory");
 }
+// 16 lanes x 32 fp32 columns in the layout of an MMA accumulator: of columns 8 j .. 8 j + 7 thread t holds row t / 4, columns 2 (t % 4) and the
+// one behind it in r[4 j], r[4 j + 1], and the same columns of row t / 4 + 8 in r[4 j + 2], r[4 j + 3].  taddr: the first of the 16 lanes.
+__device__ __forceinline__ void tmem_ld_16x32_nowait(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+// Four 8 x 8 matrices of 16-bit values, held as fragments (thread t: row t / 4, columns 2 (t % 4) and the next), stored transposed: lane
+// l gives the address of row l % 8 of transposed matrix l / 8.
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---------------------------------------------------------------- descriptors
@@ -215,7 +231,7 @@ int make_tensor_map_nhwc(CUtensorMap* m, const void* ptr, uint64_t B, uint64_t H
 // 3-D tensor map of a stack of bf16 matrices [count x rows x cols], row stride cols, matrices `stride` elements apart; boxes of 64 columns x
 // box_rows of one matrix with the 128-byte swizzle.
 int make_tensor_map_stack(CUtensorMap* m, const void* ptr, uint64_t count, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows);
-// 2-D map of a row-major bf16 matrix without gaps for stores of box_cols x box_rows from unswizzled shared memory.
-int make_tensor_map_plain(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows);
+// 2-D map of a row-major bf16 matrix without gaps for boxes of box_cols (at most 32) x box_rows with the 64-byte swizzle.
+int make_tensor_map_sw64(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows);
 bool tc_device_ok();
 }  // namespace ab
