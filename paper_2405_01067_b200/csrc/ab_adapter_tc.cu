@@ -93,16 +93,17 @@ __device__ __forceinline__ void raise(int* abort_any, int* status) {
 }
 
 // ------------------------------------------------------------------------------------------------ what a backward call prepares
-// Blocks 0 .. L-1: the 64-row slabs that have rows of adapter blockIdx.x, ascending, bit 31 set where not all rows of the slab are its own.
-// Blocks behind: T (fp32) cut into pieces, eight values a thread.
+// Blocks 0 .. L-1: the 64-row slabs that have rows of adapter blockIdx.x, ascending: (slab, which of its rows are the adapter's: 32 bits and 32
+// bits, 0).  Blocks behind: T (fp32) cut into pieces, eight values a thread.  Reads the call's inputs alone, so it runs beside the
+// kernel before it.
 constexpr int kPrepThreads = 512;
 __global__ void __launch_bounds__(kPrepThreads)
-prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict__ list, int* __restrict__ count, int nslab, const float* __restrict__ T,
-            bf16* __restrict__ P, int r, int rp, int* status) {
+prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint4* __restrict__ list, int* __restrict__ count, int nslab, const float* __restrict__ T,
+            bf16* __restrict__ P, int r, int rp, int first, int* status) {
   __shared__ int warp_cnt[kPrepThreads / 32];
-  dep_wait();
+  if (first) dep_wait();
   dep_launch();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *status = AB_OK;
+  if (first && blockIdx.x == 0 && threadIdx.x == 0) *status = AB_OK;
   if ((int)blockIdx.x >= L) {
     const int64_t step = (int64_t)(gridDim.x - L) * kPrepThreads;
     const int oct = rp / 8;
@@ -117,22 +118,24 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict_
       put_pieces(P + row * 3 * rp + k, rp, v);
     }
     fence_proxy_async_all();
+    if (!first) dep_wait();          // this kernel is done only after the one before it
     return;
   }
   const int a = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t* mine = list + (int64_t)a * nslab;
+  uint4* mine = list + (int64_t)a * nslab;
   int at = 0;
   for (int s0 = 0; s0 < nslab; s0 += kPrepThreads) {
     // a warp looks at 32 slabs, lane e keeps what slab e is
-    bool any = false, all = false;
+    unsigned lo = 0u, hi = 0u;
     const int w0 = s0 + warp * 32;
 #pragma unroll 8
     for (int e = 0; e < 32; ++e) {
       const int64_t row = (int64_t)(w0 + e) * 64 + lane;
       const bool x = row < N && ids[row] == a, y = row + 32 < N && ids[row + 32] == a;
       const unsigned vx = __ballot_sync(0xffffffffu, x), vy = __ballot_sync(0xffffffffu, y);
-      if (lane == e) { any = (vx | vy) != 0u; all = (vx & vy) == 0xffffffffu; }
+      if (lane == e) { lo = vx; hi = vy; }
     }
+    const bool any = (lo | hi) != 0u;
     const unsigned vote = __ballot_sync(0xffffffffu, any);
     if (lane == 0) warp_cnt[warp] = __popc(vote);
     __syncthreads();
@@ -143,11 +146,12 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint32_t* __restrict_
       ahead += w < warp ? c : 0;
       sum += c;
     }
-    if (any) mine[at + ahead + __popc(vote & ((1u << lane) - 1u))] = (uint32_t)(w0 + lane) | (all ? 0u : 0x80000000u);
+    if (any) mine[at + ahead + __popc(vote & ((1u << lane) - 1u))] = make_uint4((uint32_t)(w0 + lane), lo, hi, 0u);
     at += sum;
     __syncthreads();
   }
   if (threadIdx.x == 0) count[a] = at;
+  if (!first) dep_wait();
 }
 
 // ------------------------------------------------------------------------------------------------ T of rows in mixed groups
@@ -190,6 +194,7 @@ struct ProjParams {
   int first;                                // the call's first kernel
   int* status;
   // project_tc_kernel
+  int tile_ctas;                            // CTAs that have tiles
   int nk, csize, ns, slot_bytes, in_bytes, f_bytes, q_max, tmem_cols;
 };
 
@@ -203,17 +208,13 @@ __device__ __forceinline__ void put_T(const ProjParams& p, int64_t row, int k, f
   if (k < p.r) p.T[row * p.r + k] = v;
 }
 
-// Rows of tiles with more adapters than project_tc_kernel takes (there: the rows of uniform groups), or all rows where they are few.  A CTA
-// has `unit` rows and, where gridDim.y > 1, eight of the r values.  f_mn 0: a warp a value, lanes along K; f_mn 1: a thread has eight
-// neighbouring values and every so manieth row of F_a.
-__global__ void __launch_bounds__(kRowsThreads)
-rows_kernel(const ProjParams p) {
-  __shared__ float red[kRowsThreads / 32][32][8];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (p.first) dep_wait();
-  dep_launch();
-  if (p.first && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = AB_OK;
-  const int64_t row0 = (int64_t)blockIdx.x * p.unit;
+// Rows that go one by one: `unit` rows from unit * p.unit, of tiles with more adapters than project_tc_kernel takes (the rows of their mixed
+// groups), or all rows where they are few.  f_mn 0: a warp a value, lanes along K, every `parts`th round of warps; f_mn 1: a thread has
+// eight neighbouring values and every so manieth row of F_a (parts 1).  red: kWarps x 32 x 8 floats.
+template <int kWarps>
+__device__ __forceinline__ void rows_body(const ProjParams& p, int64_t unit, int part, int parts, int tid, float (*red)[32][8]) {
+  const int lane = tid & 31, warp = tid >> 5;
+  const int64_t row0 = (int64_t)unit * p.unit;
   const bool work = p.all_rows || tile_adapters(p.ids, p.N, p.L, row0 / p.tile_rows * p.tile_rows, p.tile_rows, lane, nullptr) > kMaxAd;
   if (work) {
     for (int64_t row = row0; row < row0 + p.unit && row < p.N; ++row) {
@@ -226,10 +227,9 @@ rows_kernel(const ProjParams p) {
       const float s = a < 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
       const uint4* x = reinterpret_cast<const uint4*>(p.In + row * (int64_t)p.K);
       if (a < 0) {
-        if (blockIdx.y == 0) for (int k = threadIdx.x; k < p.rp; k += kRowsThreads) put_T(p, row, k, 0.f);
+        if (part == 0) for (int k = tid; k < p.rp; k += 32 * kWarps) put_T(p, row, k, 0.f);
       } else if (!p.f_mn) {
-        const int stride = gridDim.y > 1 ? p.rp : 8;
-        for (int k = (int)blockIdx.y * 8 + warp; k < p.rp; k += stride) {
+        for (int k = part * kWarps + warp; k < p.rp; k += parts * kWarps) {
           float v = 0.f;
           if (k < p.r) {
             const uint4* f = reinterpret_cast<const uint4*>(p.F + a * p.strideF + (int64_t)k * p.K);
@@ -252,13 +252,12 @@ rows_kernel(const ProjParams p) {
             for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
           }
           if (lane == 0) put_T(p, row, k, s * v);
-          if (gridDim.y > 1) break;
         }
       } else {
         const int oct = p.r / 8;
         int op = 1;
         while (op < oct) op <<= 1;                           // at most 32
-        const int o = threadIdx.x % op, f0 = threadIdx.x / op, step = kRowsThreads / op;
+        const int o = tid % op, f0 = tid / op, step = 32 * kWarps / op;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (o < oct) {
           const bf16* F = p.F + a * p.strideF + 8 * o;
@@ -286,18 +285,26 @@ rows_kernel(const ProjParams p) {
           for (int e = 0; e < 8; ++e) red[warp][lane][e] = v[e];
         }
         __syncthreads();
-        for (int k = threadIdx.x; k < p.rp; k += kRowsThreads) {
+        for (int k = tid; k < p.rp; k += 32 * kWarps) {
           float t = 0.f;
           if (k < p.r)
-            for (int w = 0; w < kRowsThreads / 32; ++w) t += red[w][k / 8][k % 8];
+            for (int w = 0; w < kWarps; ++w) t += red[w][k / 8][k % 8];
           put_T(p, row, k, s * t);
         }
         __syncthreads();
       }
     }
   }
+}
+
+__global__ void __launch_bounds__(kRowsThreads)
+rows_kernel(const __grid_constant__ ProjParams p) {
+  __shared__ float red[kRowsThreads / 32][32][8];
+  dep_wait();
+  dep_launch();
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && p.first) *p.status = AB_OK;
+  rows_body<kRowsThreads / 32>(p, blockIdx.x, blockIdx.y, gridDim.y, threadIdx.x, red);
   fence_proxy_async_all();
-  if (!p.first) dep_wait();          // this kernel is done only after the one before it
 }
 
 // ------------------------------------------------------------------------------------------------ clusters
@@ -329,16 +336,25 @@ struct ProjBars {
 
 template <int kChunks>                    // up to 16 kChunks values of r a CTA
 __global__ void __launch_bounds__(kProjTcThreads)
-project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmF, const ProjParams p) {
+project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmF, const __grid_constant__ ProjParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   ProjBars* b = reinterpret_cast<ProjBars*>(ring + (size_t)p.ns * p.slot_bytes);
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (p.first) dep_wait();
+  dep_launch();
+  if (p.first && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = AB_OK;
+  if ((int)blockIdx.x >= p.tile_ctas) {    // behind the tiles: rows that go one by one
+    if (blockIdx.y == 0 && (int64_t)(blockIdx.x - p.tile_ctas) * p.unit < p.N)
+      rows_body<kProjTcThreads / 32>(p, blockIdx.x - p.tile_ctas, 0, 1, threadIdx.x, reinterpret_cast<float(*)[32][8]>(ring));
+    fence_proxy_async_all();
+    if (!p.first) dep_wait();
+    return;
+  }
   const int tile = (int)blockIdx.x / p.csize, rank = (int)blockIdx.x - tile * p.csize;
   const int64_t row0 = (int64_t)tile * p.tile_rows;
   const int kc0 = (int)blockIdx.y * 128, cols = p.rp - kc0 < 128 ? p.rp - kc0 : 128;
   const int per = (p.nk + p.csize - 1) / p.csize, i0 = rank * per, i1 = i0 + per < p.nk ? i0 + per : p.nk;
-  dep_launch();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&b->acc_full[i], 1); mbar_init(&b->acc_empty[i], 4); }
@@ -537,7 +553,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
     tc_fence_after();
     tmem_dealloc(tmem, p.tmem_cols);
   }
-  dep_wait();            // this kernel is done only after the one before it
+  if (!p.first) dep_wait();            // this kernel is done only after the one before it
 }
 
 // ------------------------------------------------------------------------------------------------ Out^T = W In^T + G_a T^T
@@ -1037,8 +1053,8 @@ struct GradParams {
   int slices;
   int stacked;                              // the three pieces side by side as columns of one MMA
   int nb;                                   // 64-column boxes of the small operand a slab
-  int ns, slot_bytes, bufs, tmem_cols;      // bufs: accumulators used in turn
-  const int* ids; const uint32_t* list; const int* count;
+  int ns, slot_bytes, tmem_cols;
+  const int* ids; const uint4* list; const int* count;
   int check;                                // report bad map entries (no other kernel of the call does)
   int* status;
 };
@@ -1048,11 +1064,25 @@ struct GradBars {
   int abort_any;
 };
 
+// The adapter at place `place` in the order of descending count (ties: the lower first), so that the longest sums start first.  Whole warp.
+__device__ __forceinline__ int longest(const int* __restrict__ count, int L, int place, int lane) {
+  if (L > 256) return place;               // many adapters: each is a small share of the work
+  int mine = -1;
+  for (int a0 = 0; a0 < L; a0 += 32) {
+    const int a = a0 + lane, c = a < L ? count[a] : -1;
+    int ahead = 0;
+    for (int x = 0; x < L; ++x) { const int cx = count[x]; ahead += cx > c || (cx == c && x < a) ? 1 : 0; }
+    const unsigned hit = __ballot_sync(0xffffffffu, a < L && ahead == place);
+    if (hit) mine = a0 + __ffs(hit) - 1;
+  }
+  return mine;
+}
+
 // Four slabs (256 rows) are summed in TMEM, the rest in registers, as in project_tc_kernel.
 template <int kChunks>                    // up to 16 kChunks values of r a CTA
 __global__ void __launch_bounds__(kWideThreads)
 adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_constant__ CUtensorMap tmS0,
-                       const __grid_constant__ CUtensorMap tmAct1, const __grid_constant__ CUtensorMap tmS1, const GradParams p) {
+                       const __grid_constant__ CUtensorMap tmAct1, const __grid_constant__ CUtensorMap tmS1, const __grid_constant__ GradParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   GradBars* b = reinterpret_cast<GradBars*>(ring + (size_t)p.ns * p.slot_bytes);
@@ -1062,7 +1092,7 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
   const int half = item % p.halves; item /= p.halves;
   const int tiles = p.job[0].tiles + p.job[1].tiles;
   int tile = item % tiles;
-  const int a = item / tiles, j = tile < p.job[0].tiles ? 0 : 1;
+  const int place = item / tiles, j = tile < p.job[0].tiles ? 0 : 1;
   if (j) tile -= p.job[0].tiles;
   const int f0 = tile * 128, kc0 = half * 128, kcols = p.rp - kc0 < 128 ? p.rp - kc0 : 128;
   const CUtensorMap* tmA = j ? &tmAct1 : &tmAct0;
@@ -1083,9 +1113,10 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
   tc_fence_after();
   dep_launch();
   const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
+  const int a = longest(p.count, p.L, place, lane);
   const int cnt = (int)uniform(p.count[a]), per = (cnt + p.slices - 1) / p.slices;
   const int e0 = slice * per < cnt ? slice * per : cnt, e1 = e0 + per < cnt ? e0 + per : cnt;
-  const uint32_t* list = p.list + (int64_t)a * p.nslab;
+  const uint4* list = p.list + (int64_t)a * p.nslab;
   if (p.check && blockIdx.x == 0) {
     bool bad = false;
     for (int64_t i = threadIdx.x; i < p.N; i += kWideThreads) bad |= p.ids[i] < -1 || p.ids[i] >= p.L;
@@ -1097,8 +1128,10 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
     int slot = 0, ph = 1;
     bool ok = true;
     const uint32_t tx = kABytes + p.nb * 8192;
+    uint32_t mine = 0;                     // lane l: entry l of the 32 at hand
     for (int e = e0; e < e1 && ok; ++e) {
-      const int row0 = (int)(uniform(list[e]) & 0x7fffffffu) * 64;
+      if (((e - e0) & 31) == 0) mine = e + lane < e1 ? list[e + lane].x : 0u;
+      const int row0 = (int)__shfl_sync(0xffffffffu, mine, (e - e0) & 31) * 64;
       for (int q = 0; q < pieces; ++q) {
         if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
         if (elect_one()) {
@@ -1118,10 +1151,12 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
     const uint64_t dA = smem_desc_sw128(base, 8192), dS = smem_desc_sw128(base + kABytes, 8192), slot_step = (uint64_t)(p.slot_bytes >> 4);
     int slot = 0, ph = 0;
     bool ok = true;
+    uint4 mine = make_uint4(0u, 0u, 0u, 0u);
     for (int e = e0, n = 0; e < e1 && ok; ++e, ++n) {
-      const uint32_t entry = uniform(list[e]);
-      const int flush = n / kFlush, buf = p.bufs > 1 ? flush & 1 : 0, in = n % kFlush, turn = p.bufs > 1 ? flush >> 1 : flush;
-      const bool others = entry >> 31;
+      if ((n & 31) == 0 && e + lane < e1) mine = list[e + lane];
+      const unsigned lo = __shfl_sync(0xffffffffu, mine.y, n & 31), hi = __shfl_sync(0xffffffffu, mine.z, n & 31);
+      const int flush = n / kFlush, buf = flush & 1, in = n % kFlush, turn = flush >> 1;
+      const bool others = (lo & hi) != 0xffffffffu;
       if (in == 0) {
         if (!mbar_wait_warp(&b->acc_empty[buf], (turn & 1) ^ 1)) { raise(&b->abort_any, p.status); break; }
         tc_fence_after();
@@ -1131,9 +1166,6 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
         if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
         if (others) {
           // rows that are not this adapter's: cleared in both operands, whatever they hold
-          const int64_t row = (int64_t)(entry & 0x7fffffffu) * 64 + lane;
-          const unsigned lo = __ballot_sync(0xffffffffu, row < p.N && p.ids[row] == a);
-          const unsigned hi = __ballot_sync(0xffffffffu, row + 32 < p.N && p.ids[row + 32] == a);
           uint8_t* s = ring + (size_t)slot * p.slot_bytes;
           for (int r4 = 0; r4 < 64; r4 += 4) {
             const int rr = r4 + (lane >> 3);
@@ -1169,7 +1201,7 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
     const int flushes = (e1 - e0 + kFlush - 1) / kFlush;
     bool ok = true;
     for (int n = 0; n < flushes && ok; ++n) {
-      const int buf = p.bufs > 1 ? n & 1 : 0, turn = p.bufs > 1 ? n >> 1 : n;
+      const int buf = n & 1, turn = n >> 1;
       ok = mbar_wait_warp(&b->acc_full[buf], turn & 1);
       if (!ok) { raise(&b->abort_any, p.status); break; }
       tc_fence_after();
@@ -1252,30 +1284,37 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   p.unit = 1;
   while (p.unit < p.tile_rows && tiles * p.tile_rows / p.unit > 600) p.unit *= 2;
   const int64_t units = (c.N + p.unit - 1) / p.unit;
-  const int ky = !f_mn && units <= 256 ? (rp + 7) / 8 : 1;
-  AB_TRY(launch_after(rows_kernel, dim3((unsigned)units, (unsigned)ky), (unsigned)kRowsThreads, 0, 1, c.st, p));
-  if (p.all_rows) return AB_OK;
+  if (p.all_rows) {
+    const int ky = f_mn ? 1 : (rp + kRowsThreads / 32 - 1) / (kRowsThreads / 32);
+    return launch_after(rows_kernel, dim3((unsigned)units, (unsigned)ky), (unsigned)kRowsThreads, 0, 1, c.st, p);
+  }
   const int cols = rp < 128 ? rp : 128;
   p.nk = (K + 63) / 64;
   p.in_bytes = p.tile_rows * 128;
   p.f_bytes = f_mn ? (cols + 63) / 64 * 8192 : cols * 128;
-  const int room = p.f_bytes > 8192 ? p.f_bytes : 8192;
+  const int least = f_mn ? 16384 : 8192, room = p.f_bytes > least ? p.f_bytes : least;      // two adapters of a tile at once, mostly
   p.q_max = room / p.f_bytes < 128 / cols ? room / p.f_bytes : 128 / cols;       // two accumulators in half of the columns: two CTAs an SM
   if (p.q_max > kMaxAd) p.q_max = kMaxAd;
   p.slot_bytes = p.in_bytes + room;
   if (p.slot_bytes < 16384) p.slot_bytes = 16384;          // an MMA reads 128 rows of In, loaded or not
-  // three CTAs an SM; the ring takes the parts at the end
-  const int parts = p.tile_rows * (cols + 4) * 4;
-  p.ns = 72 * 1024 / p.slot_bytes < 3 ? 3 : 72 * 1024 / p.slot_bytes;
-  if (p.ns * p.slot_bytes < parts) p.ns = (parts + p.slot_bytes - 1) / p.slot_bytes;
   p.csize = 8;
   while (p.csize > 1 && (tiles * p.csize > 2 * sms || 2 * p.csize > p.nk)) p.csize >>= 1;
+  // Up to three CTAs an SM, and no more room than for as many as there are: CTAs fill an SM before they go to the next.  The ring takes the
+  // parts at the end.
+  const int64_t each = (tiles * p.csize * ((rp + 127) / 128) + sms - 1) / sms;
+  const int parts = p.tile_rows * (cols + 4) * 4, budget = each <= 1 ? 120 * 1024 : each == 2 ? 96 * 1024 : 72 * 1024;
+  p.ns = budget / p.slot_bytes < 3 ? 3 : budget / p.slot_bytes < kMaxStages ? budget / p.slot_bytes : kMaxStages;
+  if (p.ns * p.slot_bytes < parts) p.ns = (parts + p.slot_bytes - 1) / p.slot_bytes;
   p.tmem_cols = 2 * pow2_cols(p.q_max * cols);
   CUtensorMap tmIn, tmF;
   AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.tile_rows));
   AB_TRY(stack_map(&tmF, c, F, f_mn ? K : c.r, f_mn ? c.r : K, strideF, f_mn ? 64 : cols));
-  const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + sizeof(ProjBars);
-  const dim3 grid((unsigned)(tiles * p.csize), (unsigned)((rp + 127) / 128));
+  p.tile_ctas = (int)(tiles * p.csize);
+  const int64_t ctas = tiles * p.csize + (units + p.csize - 1) / p.csize * p.csize;
+  if (ctas > 0x7fffffffll) return AB_ERR_UNSUPPORTED;
+  size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + sizeof(ProjBars);
+  if (smem < (size_t)budget) smem = budget;
+  const dim3 grid((unsigned)ctas, (unsigned)((rp + 127) / 128));
   if (cols <= 64) {
     AB_CUDA_OK(allow_smem(project_tc_kernel<4>));
     return launch_after(project_tc_kernel<4>, grid, (unsigned)kProjTcThreads, smem, p.csize, c.st, tmIn, tmF, p);
@@ -1348,7 +1387,7 @@ int grad_slices(int64_t N, int m, int n, int r, int L) {
   return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
 }
 
-struct TcWs { int* status; float *T, *U; bf16 *TP, *UP; uint32_t* list; int* count; float *pA, *pB; int slices, nslab; size_t bytes; };
+struct TcWs { int* status; float *T, *U; bf16 *TP, *UP; uint4* list; int* count; float *pA, *pB; int slices, nslab; size_t bytes; };
 TcWs tc_ws(void* ws, int64_t N, int m, int n, int r, int L) {
   Arena ar(ws, 0);
   TcWs w;
@@ -1359,7 +1398,7 @@ TcWs tc_ws(void* ws, int64_t N, int m, int n, int r, int L) {
   w.TP = ar.take_n<bf16>((size_t)N * 3 * rp);
   w.UP = ar.take_n<bf16>((size_t)N * 3 * rp);
   w.nslab = (int)((N + 63) / 64);
-  w.list = ar.take_n<uint32_t>((size_t)L * w.nslab);
+  w.list = ar.take_n<uint4>((size_t)L * w.nslab);
   w.count = ar.take_n<int>((size_t)L);
   w.slices = grad_slices(N, m, n, r, L);
   w.pA = w.slices > 1 ? ar.take_n<float>((size_t)w.slices * L * m * r) : nullptr;
@@ -1379,9 +1418,11 @@ int launch_grads(const AdapterCall& c, const void* dY, float* dA, float* dB, con
   p.nb = p.stacked ? (3 * rp + 63) / 64 : ((rp < 128 ? rp : 128) + 63) / 64;
   p.slot_bytes = kABytes + p.nb * 8192;
   const int acc = pow2_cols(p.stacked ? 3 * rp : rp < 128 ? rp : 128);
-  p.bufs = acc <= 128 ? 2 : 1;               // half of the columns: two CTAs an SM
-  p.tmem_cols = p.bufs * acc;
-  p.ns = 108 * 1024 / p.slot_bytes < kMaxStages ? 108 * 1024 / p.slot_bytes : kMaxStages;
+  // Two CTAs an SM where two accumulators leave room for another two.  (r = 64, one accumulator each and two CTAs: 58 us for the ViT groups
+  // against 45.)
+  const int ring = acc <= 128 ? 108 * 1024 : 200 * 1024;
+  p.tmem_cols = 2 * acc;
+  p.ns = ring / p.slot_bytes < kMaxStages ? ring / p.slot_bytes : kMaxStages;
   CUtensorMap act[2], small[2];
   int nj = 0;
   if (dA) {
@@ -1440,21 +1481,23 @@ int adapter_tc_forward(const AdapterCall& c, void* y, float* T_save, void* ws) {
 int adapter_tc_backward(const AdapterCall& c, const void* dY, const float* T_saved, void* dX, float* dA, float* dB, void* ws) {
   const TcWs w = tc_ws(ws, c.N, c.m, c.n, c.r, c.L);
   bool first = true;
+  if (dX || dB) {
+    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, false, w.UP, first, w.status));
+    first = false;
+  }
+  if (dA && !T_saved) {
+    AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, false, w.TP, first, w.status));
+    first = false;
+  }
+  if (dX) AB_TRY(launch_out(c, dY, c.m, true, c.B, c.strideB, dX, c.n, w.U, w.UP, w.status));
   if (dA || dB) {
     const int64_t rows = dA && T_saved ? c.N : 0;
     int64_t blocks = (rows * (pad16(c.r) / 8) + kPrepThreads - 1) / kPrepThreads;
     if (blocks > 1024) blocks = 1024;
     AB_TRY(launch_after(prep_kernel, (unsigned)(c.L + blocks), (unsigned)kPrepThreads, 0, 1, c.st, c.ids, c.N, c.L, w.list, w.count, w.nslab, T_saved, w.TP,
-                        c.r, pad16(c.r), w.status));
-    first = false;
+                        c.r, pad16(c.r), first ? 1 : 0, w.status));
+    AB_TRY(launch_grads(c, dY, dA, dB, w, !dX));
   }
-  if (dX || dB) {
-    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, false, w.UP, first, w.status));
-    first = false;
-  }
-  if (dA && !T_saved) AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, false, w.TP, first, w.status));
-  if (dX) AB_TRY(launch_out(c, dY, c.m, true, c.B, c.strideB, dX, c.n, w.U, w.UP, w.status));
-  if (dA || dB) AB_TRY(launch_grads(c, dY, dA, dB, w, !dX));
   return AB_OK;
 }
 
