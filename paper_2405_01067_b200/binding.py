@@ -341,49 +341,58 @@ def ab_adapter_workspace_bytes(x, A, B) -> int:
     return int(lib().ab_adapter_workspace_bytes(x.shape[0], m, B.shape[2], r, L, _dt(x)))
 
 
-def _adapter_ok(x, W, A, B, row_adapter, scale, dY, outs, f32):
-    """Shapes, types and places of the tensors of an adapter call.  A and B may be spaced along their first axis."""
-    if x.dim() != 2 or A.dim() != 3 or B.dim() != 3:
-        raise ValueError("x is (N, n), A (L, m, r), B (L, r, n)")
+# What the adapter calls look at in every tensor, in the order of what is cheap: a serving step is a call of 10 us on the device.
+# get_device() is -1 for a tensor that is not on a GPU.
+def _fits(what, t, shape, dtype, dev):
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {tuple(shape)} on the current device (cuda:{dev}), "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+
+
+def _adapter_ok(x, W, A, B, row_adapter, scale):
+    """Checks the inputs of an adapter call; returns (N, n, L, m, r, device).  A and B may be spaced along their first axis."""
+    if x.dim() != 2 or A.dim() != 3:
+        raise ValueError("x is (N, n), A (L, m, r)")
     N, n = x.shape
     L, m, r = A.shape
-    if B.shape != (L, r, n) or (W is not None and W.shape != (m, n)):
-        raise ValueError(f"A {tuple(A.shape)}, B {tuple(B.shape)} and W do not fit rows of {n}")
-    if row_adapter.shape != (N,) or row_adapter.dtype != torch.int32 or (scale is not None and (scale.shape != (L,) or scale.dtype != torch.float32)):
-        raise ValueError("row_adapter is int32 (N,), scale fp32 (L,)")
-    _dev_ok(x, W, row_adapter, scale, dY, *(t for t, _ in outs), *(t for t, _ in f32))
-    for t in (A, B):
-        if not t.is_cuda or (L > 0 and not t[0].is_contiguous()):
-            raise ValueError("each adapter's matrix must be a contiguous CUDA tensor")
-    for t in (W, A, B, dY) + tuple(t for t, _ in outs):
-        if t is not None and t.dtype != x.dtype:
-            raise ValueError("x, W, A, B, dY and their results have one type")
-    for t, shape in outs + f32 + (((dY, (N, m)),) if dY is not None else ()):
-        if t is not None and tuple(t.shape) != shape:
-            raise ValueError(f"expected a tensor of {shape}, got {tuple(t.shape)}")
-    dev = torch.cuda.current_device()
-    for t in (x, W, A, B, row_adapter, scale, dY) + tuple(t for t, _ in outs) + tuple(t for t, _ in f32):
-        if t is not None and t.device.index != dev:
-            raise ValueError("tensors must be on the current device")
-    for t, _ in f32:
-        if t is not None and t.dtype != torch.float32:
-            raise ValueError("T, dA and dB are fp32")
+    dt, dev = x.dtype, torch._C._cuda_getDevice()
+    _fits("x", x, (N, n), dt, dev)
+    if W is not None:
+        _fits("W", W, (m, n), dt, dev)
+    _fits("row_adapter", row_adapter, (N,), torch.int32, dev)
+    if scale is not None:
+        _fits("scale", scale, (L,), torch.float32, dev)
+    if B.shape != (L, r, n):
+        raise ValueError(f"B {tuple(B.shape)} does not fit A {tuple(A.shape)} and rows of {n}")
+    for t, cols in ((A, r), (B, n)):
+        _, s1, s2 = t.stride()
+        if t.dtype != dt or t.get_device() != dev or s1 != cols or s2 != 1:
+            if not (t.dtype == dt and t.get_device() == dev and (L == 0 or t[0].is_contiguous())):
+                raise ValueError("A and B have x's type and device, and each adapter's matrix is contiguous")
+    return N, n, L, m, r, dev
 
 
 def ab_adapter_forward(x, W, A, B, row_adapter, scale=None, y=None, T_save=None, ws=None, stream=None, save_T=False):
     """y_i = W x_i + scale_a A_a (B_a x_i) with a = row_adapter[i] (-1: W x_i alone).  x (N, n), W (m, n), A (L, m, r),
     B (L, r, n), row_adapter int32 (N,), scale fp32 (L,) or None.  Returns (y, T (N, r) fp32 or None)."""
-    N, L, m, r = x.shape[0], *A.shape
-    _adapter_ok(x, W, A, B, row_adapter, scale, None, ((y, (N, m)),), ((T_save, (N, r)),))
+    if W is None:
+        raise ValueError("the shared projection W is wanted in a forward call")
+    N, n, L, m, r, dev = _adapter_ok(x, W, A, B, row_adapter, scale)
     if y is None:
-        y = torch.empty((N, m), dtype=x.dtype, device=x.device)
-    if save_T and T_save is None:
-        T_save = torch.empty((N, r), dtype=torch.float32, device=x.device)
+        y = x.new_empty((N, m))
+    else:
+        _fits("y", y, (N, m), x.dtype, dev)
+    if T_save is not None:
+        _fits("T_save", T_save, (N, r), torch.float32, dev)
+    elif save_T:
+        T_save = x.new_empty((N, r), dtype=torch.float32)
     if ws is None:
         ws = workspace(ab_adapter_workspace_bytes(x, A, B), x.device)
-    st = lib().ab_adapter_forward(_ptr(x), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(row_adapter), _ptr(y), _ptr(T_save), N, m,
-                                  x.shape[1], r, L, A.stride(0), B.stride(0), _dt(x), _ptr(ws), ws.numel(), _stream(stream))
-    _check(st, "ab_adapter_forward")
+    st = lib().ab_adapter_forward(x.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), _ptr(scale), row_adapter.data_ptr(), y.data_ptr(),
+                                  _ptr(T_save), N, m, n, r, L, A.stride(0), B.stride(0), _dt(x), ws.data_ptr(), ws.numel(),
+                                  torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    if st != AB_OK:
+        raise AbError(st, "ab_adapter_forward")
     return y, T_save
 
 
@@ -391,20 +400,30 @@ def ab_adapter_backward(x, dY, W, A, B, row_adapter, scale=None, T_saved=None, w
                         ws=None, stream=None):
     """Gradients of ab_adapter_forward: dX (N, n), dA (L, m, r) and dB (L, r, n) in fp32; entries not in `want` are None.  T_saved is
     the T of the forward call, or None to recompute it.  W may be None where dX is not wanted."""
-    N, n, L, m, r = *x.shape, *A.shape
-    _adapter_ok(x, W, A, B, row_adapter, scale, dY, ((dX, (N, n)),), ((T_saved, (N, r)), (dA, (L, m, r)), (dB, (L, r, n))))
-    if "dX" in want and dX is None:
-        dX = torch.empty((N, n), dtype=x.dtype, device=x.device)
-    if "dA" in want and dA is None:
-        dA = torch.empty((L, m, r), dtype=torch.float32, device=x.device)
-    if "dB" in want and dB is None:
-        dB = torch.empty((L, r, n), dtype=torch.float32, device=x.device)
+    N, n, L, m, r, dev = _adapter_ok(x, W, A, B, row_adapter, scale)
+    _fits("dY", dY, (N, m), x.dtype, dev)
+    if T_saved is not None:
+        _fits("T_saved", T_saved, (N, r), torch.float32, dev)
+    if dX is not None:
+        _fits("dX", dX, (N, n), x.dtype, dev)
+    elif "dX" in want:
+        dX = x.new_empty((N, n))
+    if dA is not None:
+        _fits("dA", dA, (L, m, r), torch.float32, dev)
+    elif "dA" in want:
+        dA = x.new_empty((L, m, r), dtype=torch.float32)
+    if dB is not None:
+        _fits("dB", dB, (L, r, n), torch.float32, dev)
+    elif "dB" in want:
+        dB = x.new_empty((L, r, n), dtype=torch.float32)
     if ws is None:
         ws = workspace(ab_adapter_workspace_bytes(x, A, B), x.device)
-    st = lib().ab_adapter_backward(_ptr(x), _ptr(dY), _ptr(W), _ptr(A), _ptr(B), _ptr(scale), _ptr(row_adapter), _ptr(T_saved), _ptr(dX),
-                                   _ptr(dA), _ptr(dB), N, m, n, r, L, A.stride(0), B.stride(0), _dt(x), _ptr(ws), ws.numel(),
-                                   _stream(stream))
-    _check(st, "ab_adapter_backward")
+    st = lib().ab_adapter_backward(x.data_ptr(), dY.data_ptr(), _ptr(W), A.data_ptr(), B.data_ptr(), _ptr(scale), row_adapter.data_ptr(),
+                                   _ptr(T_saved), _ptr(dX), _ptr(dA), _ptr(dB), N, m, n, r, L, A.stride(0), B.stride(0), _dt(x),
+                                   ws.data_ptr(), ws.numel(),
+                                   torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    if st != AB_OK:
+        raise AbError(st, "ab_adapter_backward")
     return dX, dA, dB
 
 

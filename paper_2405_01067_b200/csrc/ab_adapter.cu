@@ -10,6 +10,7 @@
 #include <string.h>
 
 #include "ab_adapter.cuh"
+#include "ab_tc_ptx.cuh"
 
 namespace ab {
 namespace {
@@ -27,98 +28,165 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// T[i][k] = s_a sum_j In[i][j] F_a(k, j), one block a row; F_a(k, j) at F + a strideF + k f_k + j f_j, one of f_k, f_j is 1: the lanes run
-// along that one.  Partial sums of a lane in fp32, joined by a tree.
-template <typename TI>
+// T[i][k] = s_a sum_j In[i][j] F_a(k, j), kRB rows a block; F_a(k, j) at F + a strideF + k f_k + j f_j, one of f_k, f_j is 1: the lanes run
+// along that one.  Neighbouring rows mostly have the same adapter: F_a is then read once for all of the block's rows (1531 rows, r 12, 777
+// wide: 12.8 us a row a block).  Partial sums of a lane in fp32, joined by a tree: the bits of a row do not depend on its neighbours.
+template <typename TI, int kRB>
 __global__ void __launch_bounds__(kProjThreads)
 project_kernel(const TI* __restrict__ In, const TI* __restrict__ F, int64_t strideF, int64_t f_k, int64_t f_j,
-               const float* __restrict__ scale, const int* __restrict__ ids, float* __restrict__ T, int K, int r, int L, int* status) {
-  __shared__ float part[kProjThreads];
-  const int64_t row = blockIdx.x;
-  if (row == 0 && threadIdx.x == 0) *status = AB_OK;
-  const int a = ids[row];
-  float* Trow = T + row * r;
-  if (a < 0 || a >= L) {
-    for (int k = threadIdx.x; k < r; k += kProjThreads) Trow[k] = 0.f;
-    return;
+               const float* __restrict__ scale, const int* __restrict__ ids, float* __restrict__ T, int64_t N, int K, int r, int L, int first,
+               int* status) {
+  __shared__ float part[kRB][kProjThreads];
+  tc::dep_wait();
+  tc::dep_launch();
+  const int64_t row0 = (int64_t)blockIdx.x * kRB;
+  if (first && row0 == 0 && threadIdx.x == 0) *status = AB_OK;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int id[kRB];
+#pragma unroll
+  for (int i = 0; i < kRB; ++i) {
+    const int a = row0 + i < N ? ids[row0 + i] : -1;
+    id[i] = a >= 0 && a < L ? a : -1;
+    if (id[i] < 0 && row0 + i < N)
+      for (int k = threadIdx.x; k < r; k += kProjThreads) T[(row0 + i) * r + k] = 0.f;
   }
-  const float s = scale ? scale[a] : 1.f;
-  const TI* x = In + row * (int64_t)K;
-  const TI* Fa = F + a * strideF;
-  if (f_j == 1) {
-    for (int k = threadIdx.x >> 5; k < r; k += kProjThreads / 32) {
-      const TI* f = Fa + k * f_k;
-      float v = 0.f;
-      for (int j = threadIdx.x & 31; j < K; j += 32) v = fmaf(to_f32(x[j]), to_f32(f[j]), v);
-      v = warp_sum(v);
-      if ((threadIdx.x & 31) == 0) Trow[k] = s * v;
+#pragma unroll 1
+  for (int h = 0; h < kRB; ++h) {            // a pass for each adapter of the block
+    int a = -1;
+    unsigned mine = 0;
+#pragma unroll
+    for (int i = 0; i < kRB; ++i) {
+      bool seen = false;
+#pragma unroll
+      for (int e = 0; e < kRB; ++e) seen |= e < h && id[e] == id[i];
+      if (i == h && !seen) a = id[i];
     }
-    return;
-  }
-  int kt = 1;
-  while (kt < r && kt < kProjThreads) kt <<= 1;
-  const int jp = kProjThreads / kt, kk = threadIdx.x % kt, j0 = threadIdx.x / kt;
-  for (int k0 = 0; k0 < r; k0 += kt) {
-    const int k = k0 + kk;
-    float v = 0.f;
-    if (k < r)
-      for (int j = j0; j < K; j += jp) v = fmaf(to_f32(x[j]), to_f32(Fa[j * f_j + k]), v);
-    part[threadIdx.x] = v;
-    __syncthreads();
-    for (int h = jp >> 1; h > 0; h >>= 1) {
-      if (j0 < h) part[threadIdx.x] += part[threadIdx.x + h * kt];
+    if (a < 0) continue;
+#pragma unroll
+    for (int i = 0; i < kRB; ++i) mine |= id[i] == a ? 1u << i : 0u;
+    const float s = scale ? scale[a] : 1.f;
+    const TI* x = In + row0 * (int64_t)K;
+    const TI* Fa = F + a * strideF;
+    const int last = (int)(N - row0 < kRB ? N - row0 : kRB) - 1;
+    if (f_j == 1) {
+      for (int k = warp; k < r; k += kProjThreads / 32) {
+        const TI* f = Fa + k * f_k;
+        float v[kRB];
+#pragma unroll
+        for (int i = 0; i < kRB; ++i) v[i] = 0.f;
+#pragma unroll 4
+        for (int j = lane; j < K; j += 32) {
+          const float w = to_f32(f[j]);
+#pragma unroll
+          for (int i = 0; i < kRB; ++i) v[i] = fmaf(to_f32(x[(int64_t)(i < last ? i : last) * K + j]), w, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kRB; ++i) {
+          const float t = warp_sum(v[i]);
+          if (lane == 0 && ((mine >> i) & 1u)) T[(row0 + i) * r + k] = s * t;
+        }
+      }
+      continue;
+    }
+    int kt = 1;
+    while (kt < r && kt < kProjThreads) kt <<= 1;
+    const int jp = kProjThreads / kt, kk = threadIdx.x % kt, j0 = threadIdx.x / kt;
+    for (int k0 = 0; k0 < r; k0 += kt) {
+      const int k = k0 + kk;
+      float v[kRB];
+#pragma unroll
+      for (int i = 0; i < kRB; ++i) v[i] = 0.f;
+      if (k < r) {
+#pragma unroll 4
+        for (int j = j0; j < K; j += jp) {
+          const float w = to_f32(Fa[j * f_j + k]);
+#pragma unroll
+          for (int i = 0; i < kRB; ++i) v[i] = fmaf(to_f32(x[(int64_t)(i < last ? i : last) * K + j]), w, v[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kRB; ++i) part[i][threadIdx.x] = v[i];
+      __syncthreads();
+      for (int g = jp >> 1; g > 0; g >>= 1) {
+        if (j0 < g) {
+#pragma unroll
+          for (int i = 0; i < kRB; ++i) part[i][threadIdx.x] += part[i][threadIdx.x + g * kt];
+        }
+        __syncthreads();
+      }
+      if (j0 == 0 && k < r) {
+#pragma unroll
+        for (int i = 0; i < kRB; ++i)
+          if ((mine >> i) & 1u) T[(row0 + i) * r + k] = s * part[i][kk];
+      }
       __syncthreads();
     }
-    if (j0 == 0 && k < r) Trow[k] = s * part[kk];
-    __syncthreads();
   }
 }
 
-// out[i][c] = base[i][c] + sum_k T[i][k] G_a(c, k), rounded once; G_a(c, k) at G + a strideG + c g_c + k g_k.  base may be out itself
-// (fp32).  A map entry that is neither an adapter nor -1 is reported.
-constexpr int kDeltaRows = 8, kDeltaCols = 256, kDeltaK = 64;
-template <typename TI, typename TO>
+// out[i][c] = sum over the slices of base + sum_k T[i][k] G_a(c, k), rounded once; G_a(c, k) at G + a strideG + c g_c + k g_k.  base may be
+// out itself (fp32, one slice).  A map entry that is neither an adapter nor -1 is reported.  A thread has a column and kRD rows; sixteen
+// of G's values at a time are in registers, and stay there while the next row has the same adapter.
+constexpr int kDeltaCols = 256, kDeltaK = 64;
+template <typename TI, typename TO, int kRD>
 __global__ void __launch_bounds__(kDeltaCols)
-delta_kernel(const float* base, const float* __restrict__ T, const TI* __restrict__ G, int64_t strideG, int64_t g_c, int64_t g_k,
+delta_kernel(const float* base, int slices, const float* __restrict__ T, const TI* __restrict__ G, int64_t strideG, int64_t g_c, int64_t g_k,
              const int* __restrict__ ids, TO* out, int64_t N, int P, int r, int L, int* status) {
-  __shared__ float Ts[kDeltaRows][kDeltaK];
-  __shared__ int id[kDeltaRows];
-  const int64_t row0 = (int64_t)blockIdx.x * kDeltaRows;
-  const int c = blockIdx.y * kDeltaCols + threadIdx.x;
-  const int rows = (int)(N - row0 < kDeltaRows ? N - row0 : kDeltaRows);
-  if (threadIdx.x < rows) {
-    const int a = ids[row0 + threadIdx.x];
+  __shared__ float Ts[kRD][kDeltaK];
+  __shared__ int id[kRD];
+  tc::dep_wait();
+  tc::dep_launch();
+  const int64_t row0 = (int64_t)blockIdx.x * kRD;
+  const int c = blockIdx.y * kDeltaCols + threadIdx.x, cc = c < P ? c : P - 1;
+  const int rows = (int)(N - row0 < kRD ? N - row0 : kRD);
+  if (threadIdx.x < kRD) {
+    const int a = threadIdx.x < rows ? ids[row0 + threadIdx.x] : -1;
     if (a < -1 || a >= L) atomicExch(status, (int)AB_ERR_INVALID_ARG);
     id[threadIdx.x] = a >= 0 && a < L ? a : -1;
   }
-  float acc[kDeltaRows];
+  float acc[kRD];
 #pragma unroll
-  for (int i = 0; i < kDeltaRows; ++i) acc[i] = 0.f;
+  for (int i = 0; i < kRD; ++i) acc[i] = 0.f;
   for (int k0 = 0; k0 < r; k0 += kDeltaK) {
     const int kn = r - k0 < kDeltaK ? r - k0 : kDeltaK;
     __syncthreads();
     for (int e = threadIdx.x; e < rows * kDeltaK; e += kDeltaCols)
-      if (e % kDeltaK < kn) Ts[e / kDeltaK][e % kDeltaK] = T[(row0 + e / kDeltaK) * r + k0 + e % kDeltaK];
+      Ts[e / kDeltaK][e % kDeltaK] = e % kDeltaK < kn ? T[(row0 + e / kDeltaK) * r + k0 + e % kDeltaK] : 0.f;
     __syncthreads();
-    if (c < P) {
+    for (int k1 = 0; k1 < kn; k1 += 16) {
+      float g[16];
+      int have = -1;
 #pragma unroll
-      for (int i = 0; i < kDeltaRows; ++i) {
+      for (int i = 0; i < kRD; ++i) {
         if (i >= rows || id[i] < 0) continue;
-        const TI* g = G + id[i] * strideG + c * g_c + k0 * g_k;
+        if (id[i] != have) {
+          have = id[i];
+          const TI* q = G + have * strideG + cc * g_c + (k0 + k1) * g_k;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) g[e] = k1 + e < kn ? to_f32(q[e * g_k]) : 0.f;
+        }
         float v = acc[i];
-        for (int k = 0; k < kn; ++k) v = fmaf(Ts[i][k], to_f32(g[k * g_k]), v);
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const float4 t = *reinterpret_cast<const float4*>(&Ts[i][k1 + e]);
+          v = fmaf(t.x, g[e], v); v = fmaf(t.y, g[e + 1], v); v = fmaf(t.z, g[e + 2], v); v = fmaf(t.w, g[e + 3], v);
+        }
         acc[i] = v;
       }
     }
   }
   if (c >= P) return;
+  float v[kRD];
 #pragma unroll
-  for (int i = 0; i < kDeltaRows; ++i) {
-    if (i >= rows) continue;
-    const int64_t o = (row0 + i) * P + c;
-    if (id[i] >= 0) from_f32(out[o], base[o] + acc[i]);
-    else if ((const void*)base != (const void*)out) from_f32(out[o], base[o]);
+  for (int i = 0; i < kRD; ++i) v[i] = i < rows ? base[(row0 + i) * P + c] : 0.f;
+  for (int s = 1; s < slices; ++s) {
+    const float* q = base + s * N * P + row0 * P + c;
+#pragma unroll
+    for (int i = 0; i < kRD; ++i) v[i] += i < rows ? q[(int64_t)i * P] : 0.f;
   }
+#pragma unroll
+  for (int i = 0; i < kRD; ++i)
+    if (i < rows) from_f32(out[(row0 + i) * P + c], id[i] >= 0 ? v[i] + acc[i] : v[i]);
 }
 
 // The rows of each adapter in ascending order: adapter a's are order[start[a] .. start[a] + count[a]).  One block an adapter: it counts the
@@ -129,6 +197,8 @@ list_rows_kernel(const int* __restrict__ ids, int64_t N, int L, int* __restrict_
                  int64_t* __restrict__ count, int* status, int clear_status) {
   __shared__ int warp_cnt[kListThreads / 32];
   __shared__ int64_t before;
+  tc::dep_wait();
+  tc::dep_launch();
   const int a = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long less = 0;
   int bad = 0;
@@ -166,18 +236,26 @@ list_rows_kernel(const int* __restrict__ ids, int64_t N, int L, int* __restrict_
   if (threadIdx.x == 0) { start[a] = first; count[a] = at - first; }
 }
 
-// D_a(f, k) = sum over the rows i of adapter a of In[i][f] S[i][k], at D + a strideD + f d_f + k d_k.  A block has 64 values of f and 32
-// of k of one adapter; rows in their order, 32 at a time in fp32, those sums in fp64: a long sum loses nothing that fp32 shows.
+// D_a(f, k) = sum over the rows i of adapter a of In[i][f] S[i][k], at D + a strideD + f d_f + k d_k, for one or two such gradients.  A block
+// has 64 values of f and 32 of k of one adapter; rows in their order, 32 at a time in fp32, those sums in fp64: a long sum loses
+// nothing that fp32 shows.
 constexpr int kGF = 64, kGK = 32, kGR = 32;
+struct GradSide { const void* In; int P, tiles; const float* S; float* D; int64_t strideD, d_f, d_k; };
+struct GradSides { GradSide side[2]; };
 template <typename TI>
 __global__ void __launch_bounds__(256)
-adapter_grad_kernel(const TI* __restrict__ In, int P, const float* __restrict__ S, int r, const int* __restrict__ order,
-                    const int64_t* __restrict__ start, const int64_t* __restrict__ count, float* __restrict__ D, int64_t strideD, int64_t d_f,
-                    int64_t d_k) {
+adapter_grad_kernel(const __grid_constant__ GradSides sides, int r, const int* __restrict__ order, const int64_t* __restrict__ start,
+                    const int64_t* __restrict__ count) {
   __shared__ float Is[kGR][kGF];
   __shared__ float4 Ss[kGR][kGK / 4];
   __shared__ int rows[kGR];
-  const int f0 = blockIdx.x * kGF, k0 = blockIdx.y * kGK, a = blockIdx.z;
+  tc::dep_wait();
+  tc::dep_launch();
+  const int second = (int)blockIdx.x >= sides.side[0].tiles ? 1 : 0;
+  const GradSide& w = sides.side[second];
+  const TI* In = static_cast<const TI*>(w.In);
+  const int P = w.P;
+  const int f0 = ((int)blockIdx.x - (second ? sides.side[0].tiles : 0)) * kGF, k0 = blockIdx.y * kGK, a = blockIdx.z;
   const int f = threadIdx.x % kGF, kq = threadIdx.x / kGF;      // this thread: column f, values 8 kq .. 8 kq + 7
   const int64_t n = count[a];
   const int* mine = order + start[a];
@@ -189,18 +267,21 @@ adapter_grad_kernel(const TI* __restrict__ In, int P, const float* __restrict__ 
     __syncthreads();
     if (threadIdx.x < rn) rows[threadIdx.x] = mine[i0 + threadIdx.x];
     __syncthreads();
-    for (int e = threadIdx.x; e < rn * kGF; e += 256) {
-      const int q = e / kGF, c = e % kGF;
-      Is[q][c] = f0 + c < P ? to_f32(In[(int64_t)rows[q] * P + f0 + c]) : 0.f;
+#pragma unroll
+    for (int u = 0; u < kGR * kGF / 256; ++u) {
+      const int e = threadIdx.x + u * 256, q = e / kGF, c = e % kGF;
+      Is[q][c] = q < rn && f0 + c < P ? to_f32(In[(int64_t)rows[q] * P + f0 + c]) : 0.f;
     }
-    for (int e = threadIdx.x; e < rn * kGK; e += 256) {
-      const int q = e / kGK, c = e % kGK;
-      reinterpret_cast<float*>(&Ss[q][0])[c] = k0 + c < r ? S[(int64_t)rows[q] * r + k0 + c] : 0.f;
+#pragma unroll
+    for (int u = 0; u < kGR * kGK / 256; ++u) {
+      const int e = threadIdx.x + u * 256, q = e / kGK, c = e % kGK;
+      reinterpret_cast<float*>(&Ss[q][0])[c] = q < rn && k0 + c < r ? w.S[(int64_t)rows[q] * r + k0 + c] : 0.f;
     }
     __syncthreads();
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll 8
     for (int q = 0; q < rn; ++q) {
       const float xi = Is[q][f];
       const float4 s0 = Ss[q][2 * kq], s1 = Ss[q][2 * kq + 1];
@@ -211,15 +292,34 @@ adapter_grad_kernel(const TI* __restrict__ In, int P, const float* __restrict__ 
     for (int e = 0; e < 8; ++e) acc[e] += (double)v[e];
   }
   if (f0 + f >= P) return;
-  float* d = D + a * strideD + (f0 + f) * d_f;
+  float* d = w.D + a * w.strideD + (f0 + f) * w.d_f;
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    if (k0 + 8 * kq + e < r) d[(k0 + 8 * kq + e) * d_k] = (float)acc[e];
+    if (k0 + 8 * kq + e < r) d[(k0 + 8 * kq + e) * w.d_k] = (float)acc[e];
 }
 
 typedef AdapterCall Call;
 
-// Workspace of the general path: status word, T, U, base of a bf16 result in fp32, the adapters' rows
+// The shared product in fp32 goes to the tensor cores as six bf16 terms (one where the storage is bf16), which cut their sums off at every
+// step: reductions above 768 are cut into slices (777: 7.4e-7 of the result in one, 5e-7 is what fp32 fused multiply-adds lose;
+// 3900: 4.2e-6), whose sums delta_kernel adds.  Above that as many slices as leave the busiest SM the fewest slabs of 64, a tile's start
+// and end counted as two, a slice's way through memory as one.
+int base_slices(int64_t N, int P, int K) {
+  const int sms = sm_count() > 0 ? sm_count() : 148;
+  const int least = (K + 767) / 768 < kSplitFew ? (K + 767) / 768 : kSplitFew;
+  const int64_t tiles = (N + 127) / 128 * ((P + 127) / 128);
+  int best = least;
+  int64_t best_t = INT64_MAX;
+  for (int s = least; s <= kSplitFew && (s == least || s * 128 <= K); ++s) {
+    const int64_t t = (tiles * s + sms - 1) / sms * ((K + 64 * s - 1) / (64 * s) + 2) + s;
+    if (t < best_t) { best_t = t; best = s; }
+  }
+  return best;
+}
+// Small products stay on the fp32 pipes (128 x 512 x 256: 11.6 us against 12.0, and no slices)
+bool base_small(const Call& c, int P, int K) { return c.dt == AB_F32 && gemm_small_pays(c.N, P, K); }
+
+// Workspace of the general path: status word, T, U, the shared product, the adapters' rows
 struct GeneralWs { int* status; float *T, *U, *base; int* order; int64_t *start, *count; size_t bytes; };
 GeneralWs general_ws(void* ws, int64_t N, int m, int n, int r, int L, int dt) {
   Arena ar(ws, 0);
@@ -227,7 +327,10 @@ GeneralWs general_ws(void* ws, int64_t N, int m, int n, int r, int L, int dt) {
   w.status = ar.take_n<int>(64);
   w.T = ar.take_n<float>((size_t)N * r);
   w.U = ar.take_n<float>((size_t)N * r);
-  w.base = dt == AB_BF16 ? ar.take_n<float>((size_t)N * (m > n ? m : n)) : nullptr;
+  const int sy = base_slices(N, m, n), sx = base_slices(N, n, m);
+  const size_t y = (size_t)sy * m, x = (size_t)sx * n;
+  const bool none = dt == AB_F32 && sy == 1 && sx == 1;      // a slice by itself lies in an fp32 result
+  w.base = none ? nullptr : ar.take_n<float>((size_t)N * (x > y ? x : y));
   w.order = ar.take_n<int>((size_t)N);
   w.start = ar.take_n<int64_t>((size_t)L);
   w.count = ar.take_n<int64_t>((size_t)L);
@@ -235,68 +338,96 @@ GeneralWs general_ws(void* ws, int64_t N, int m, int n, int r, int L, int dt) {
   return w;
 }
 
-int project(const Call& c, const void* In, int K, const void* F, int64_t strideF, int64_t f_k, int64_t f_j, float* T, int* status) {
+template <typename TI, int kRB>
+int launch_project(const Call& c, const void* In, int K, const void* F, int64_t strideF, int64_t f_k, int64_t f_j, float* T, bool first, int* status) {
+  return launch_after(project_kernel<TI, kRB>, (unsigned)((c.N + kRB - 1) / kRB), (unsigned)kProjThreads, 0, 1, c.st, static_cast<const TI*>(In),
+                      static_cast<const TI*>(F), strideF, f_k, f_j, c.scale, c.ids, T, c.N, K, c.r, c.L, first ? 1 : 0, status);
+}
+int project(const Call& c, const void* In, int K, const void* F, int64_t strideF, int64_t f_k, int64_t f_j, float* T, bool first, int* status) {
+  const bool four = c.N >= 1024;             // fewer rows: a block each fills the device better
   if (c.dt == AB_F32)
-    project_kernel<float><<<(unsigned)c.N, kProjThreads, 0, c.st>>>(static_cast<const float*>(In), static_cast<const float*>(F), strideF, f_k, f_j,
-                                                                    c.scale, c.ids, T, K, c.r, c.L, status);
-  else
-    project_kernel<bf16><<<(unsigned)c.N, kProjThreads, 0, c.st>>>(static_cast<const bf16*>(In), static_cast<const bf16*>(F), strideF, f_k, f_j,
-                                                                   c.scale, c.ids, T, K, c.r, c.L, status);
-  AB_LAUNCH_OK();
-  return AB_OK;
+    return four ? launch_project<float, 4>(c, In, K, F, strideF, f_k, f_j, T, first, status)
+                : launch_project<float, 1>(c, In, K, F, strideF, f_k, f_j, T, first, status);
+  return four ? launch_project<bf16, 4>(c, In, K, F, strideF, f_k, f_j, T, first, status)
+              : launch_project<bf16, 1>(c, In, K, F, strideF, f_k, f_j, T, first, status);
 }
 
-int add_delta(const Call& c, const float* base, const float* T, const void* G, int64_t strideG, int64_t g_c, int64_t g_k, void* out, int P,
-              int* status) {
-  const dim3 grid((unsigned)((c.N + kDeltaRows - 1) / kDeltaRows), (unsigned)((P + kDeltaCols - 1) / kDeltaCols));
-  if (c.dt == AB_F32)
-    delta_kernel<float, float><<<grid, kDeltaCols, 0, c.st>>>(base, T, static_cast<const float*>(G), strideG, g_c, g_k, c.ids, static_cast<float*>(out),
-                                                              c.N, P, c.r, c.L, status);
-  else
-    delta_kernel<bf16, bf16><<<grid, kDeltaCols, 0, c.st>>>(base, T, static_cast<const bf16*>(G), strideG, g_c, g_k, c.ids, static_cast<bf16*>(out),
-                                                            c.N, P, c.r, c.L, status);
-  AB_LAUNCH_OK();
-  return AB_OK;
+template <typename T16, int kRD>
+int launch_delta(const Call& c, const float* base, int slices, const float* T, const void* G, int64_t strideG, int64_t g_c, int64_t g_k, void* out,
+                 int P, int* status) {
+  const dim3 grid((unsigned)((c.N + kRD - 1) / kRD), (unsigned)((P + kDeltaCols - 1) / kDeltaCols));
+  return launch_after(delta_kernel<T16, T16, kRD>, grid, (unsigned)kDeltaCols, 0, 1, c.st, base, slices, T, static_cast<const T16*>(G), strideG, g_c,
+                      g_k, c.ids, static_cast<T16*>(out), c.N, P, c.r, c.L, status);
 }
 
-int grad(const Call& c, const GeneralWs& w, const void* In, int P, const float* S, float* D, int64_t strideD, int64_t d_f, int64_t d_k) {
+// out = In W^T (W: P x K, row-major) or In W (W: K x P), and T's part
+int shared_and_delta(const Call& c, const void* In, int K, bool w_mn, const float* T, const void* G, int64_t strideG, int64_t g_c, int64_t g_k,
+                     void* out, int P, const GeneralWs& w) {
+  const int sms = sm_count() > 0 ? sm_count() : 148;
+  float* base = w.base;
+  int slices = 1;
+  if (base_small(c, P, K) || !gemm_tc_available() || c.N > 0x3fffffff) {
+    if (c.dt == AB_F32) base = static_cast<float*>(out);
+    AB_TRY(gemm_simt(In, c.dt, K, 1, c.W, c.dt, w_mn ? P : 1, w_mn ? 1 : K, base, AB_F32, P, c.N, P, K, c.st));
+  } else {
+    slices = base_slices(c.N, P, K);
+    if (c.dt == AB_F32 && slices == 1) base = static_cast<float*>(out);
+    const int per = ((K + slices - 1) / slices + 63) / 64 * 64;
+    const int64_t e = (int64_t)dtype_size(c.dt);
+    SplitGemm p[kSplitFew];
+    memset(p, 0, sizeof(p));
+    int n = 0;
+    for (int k0 = 0; k0 < K; k0 += per, ++n) {
+      p[n].A = static_cast<const char*>(In) + k0 * e; p[n].lda = K;
+      p[n].B = static_cast<const char*>(c.W) + (w_mn ? (int64_t)k0 * P : (int64_t)k0) * e; p[n].ldb = w_mn ? P : K; p[n].b_mn = w_mn ? 1 : 0;
+      p[n].C = base + (int64_t)n * c.N * P; p[n].ldc = P;
+      p[n].M = (int)c.N; p[n].N = P; p[n].K = K - k0 < per ? K - k0 : per;
+    }
+    slices = n;
+    AB_TRY(gemm_split_few(p, n, c.dt == AB_BF16, w.status, c.st));
+  }
+  // sixteen rows a block where that still gives every SM two blocks
+  const int64_t blocks = (c.N + 15) / 16 * ((P + kDeltaCols - 1) / kDeltaCols);
+  if (c.dt == AB_F32)
+    return blocks >= 2 * sms ? launch_delta<float, 16>(c, base, slices, T, G, strideG, g_c, g_k, out, P, w.status)
+                             : launch_delta<float, 2>(c, base, slices, T, G, strideG, g_c, g_k, out, P, w.status);
+  return blocks >= 2 * sms ? launch_delta<bf16, 16>(c, base, slices, T, G, strideG, g_c, g_k, out, P, w.status)
+                           : launch_delta<bf16, 2>(c, base, slices, T, G, strideG, g_c, g_k, out, P, w.status);
+}
+
+int grads(const Call& c, const GeneralWs& w, const void* dY, const float* T, float* dA, float* dB) {
+  GradSides s;
+  memset(&s, 0, sizeof(s));
+  int n = 0;
+  if (dA) s.side[n++] = GradSide{dY, c.m, (c.m + kGF - 1) / kGF, T, dA, (int64_t)c.m * c.r, c.r, 1};
+  if (dB) s.side[n++] = GradSide{c.x, c.n, (c.n + kGF - 1) / kGF, w.U, dB, (int64_t)c.r * c.n, 1, c.n};
+  const unsigned tiles = (unsigned)(s.side[0].tiles + s.side[1].tiles);
   for (int a0 = 0; a0 < c.L; a0 += 65535) {
-    const dim3 grid((unsigned)((P + kGF - 1) / kGF), (unsigned)((c.r + kGK - 1) / kGK), (unsigned)(c.L - a0 < 65535 ? c.L - a0 : 65535));
-    if (c.dt == AB_F32)
-      adapter_grad_kernel<float><<<grid, 256, 0, c.st>>>(static_cast<const float*>(In), P, S, c.r, w.order, w.start + a0, w.count + a0, D + a0 * strideD,
-                                                         strideD, d_f, d_k);
-    else
-      adapter_grad_kernel<bf16><<<grid, 256, 0, c.st>>>(static_cast<const bf16*>(In), P, S, c.r, w.order, w.start + a0, w.count + a0, D + a0 * strideD,
-                                                        strideD, d_f, d_k);
-    AB_LAUNCH_OK();
+    const dim3 grid(tiles, (unsigned)((c.r + kGK - 1) / kGK), (unsigned)(c.L - a0 < 65535 ? c.L - a0 : 65535));
+    const int* order = w.order;
+    const int64_t *start = w.start + a0, *count = w.count + a0;
+    if (c.dt == AB_F32) AB_TRY(launch_after(adapter_grad_kernel<float>, grid, 256u, 0, 1, c.st, s, c.r, order, start, count));
+    else AB_TRY(launch_after(adapter_grad_kernel<bf16>, grid, 256u, 0, 1, c.st, s, c.r, order, start, count));
+    for (int i = 0; i < n; ++i) s.side[i].D += 65535 * s.side[i].strideD;
   }
   return AB_OK;
 }
 
 int general_forward(const Call& c, void* y, float* T_save, const GeneralWs& w) {
   float* T = T_save ? T_save : w.T;
-  AB_TRY(project(c, c.x, c.n, c.B, c.strideB, c.n, 1, T, w.status));
-  float* base = c.dt == AB_F32 ? static_cast<float*>(y) : w.base;
-  AB_TRY(gemm_simt(c.x, c.dt, c.n, 1, c.W, c.dt, 1, c.n, base, AB_F32, c.m, c.N, c.m, c.n, c.st));
-  return add_delta(c, base, T, c.A, c.strideA, c.r, 1, y, c.m, w.status);
+  AB_TRY(project(c, c.x, c.n, c.B, c.strideB, c.n, 1, T, true, w.status));
+  return shared_and_delta(c, c.x, c.n, false, T, c.A, c.strideA, c.r, 1, y, c.m, w);
 }
 
 int general_backward(const Call& c, const void* dY, const float* T_saved, void* dX, float* dA, float* dB, const GeneralWs& w) {
-  const bool want_U = dX || dB;
-  if (want_U) AB_TRY(project(c, dY, c.m, c.A, c.strideA, 1, c.r, w.U, w.status));
-  if (dA && !T_saved) AB_TRY(project(c, c.x, c.n, c.B, c.strideB, c.n, 1, w.T, w.status));
-  if (dX) {
-    float* base = c.dt == AB_F32 ? static_cast<float*>(dX) : w.base;
-    AB_TRY(gemm_simt(dY, c.dt, c.m, 1, c.W, c.dt, c.n, 1, base, AB_F32, c.n, c.N, c.n, c.m, c.st));
-    AB_TRY(add_delta(c, base, w.U, c.B, c.strideB, 1, c.n, dX, c.n, w.status));
-  }
+  bool first = true;
+  if (dX || dB) { AB_TRY(project(c, dY, c.m, c.A, c.strideA, 1, c.r, w.U, first, w.status)); first = false; }
+  if (dA && !T_saved) { AB_TRY(project(c, c.x, c.n, c.B, c.strideB, c.n, 1, w.T, first, w.status)); first = false; }
+  if (dX) AB_TRY(shared_and_delta(c, dY, c.m, true, w.U, c.B, c.strideB, 1, c.n, dX, c.n, w));
   if (!dA && !dB) return AB_OK;
-  list_rows_kernel<<<(unsigned)c.L, kListThreads, 0, c.st>>>(c.ids, c.N, c.L, w.order, w.start, w.count, w.status,
-                                                             !want_U && (!dA || T_saved) ? 1 : 0);
-  AB_LAUNCH_OK();
-  if (dA) AB_TRY(grad(c, w, dY, c.m, T_saved ? T_saved : w.T, dA, (int64_t)c.m * c.r, c.r, 1));
-  if (dB) AB_TRY(grad(c, w, c.x, c.n, w.U, dB, (int64_t)c.r * c.n, 1, c.n));
-  return AB_OK;
+  AB_TRY(launch_after(list_rows_kernel, (unsigned)c.L, (unsigned)kListThreads, 0, 1, c.st, c.ids, c.N, c.L, w.order, w.start, w.count, w.status,
+                      first ? 1 : 0));
+  return grads(c, w, dY, T_saved ? T_saved : w.T, dA, dB);
 }
 
 int check_args(const Call& c) {

@@ -608,11 +608,11 @@ __device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int6
   const int ff = f < p.P ? f : p.P - 1;       // a lane past the last feature reads what its neighbour reads
   const int rows = (int)(end - row0 < kG ? end - row0 : kG);
   const int id = lane < rows ? clean_id(p.ids[row0 + lane], p.L) : -1;
-  const int before = __shfl_up_sync(0xffffffffu, id, 1);
-  const unsigned heads = __ballot_sync(0xffffffffu, id >= 0 && (lane == 0 || id != before));      // first rows of runs
   const unsigned live = __ballot_sync(0xffffffffu, id >= 0);
-  const int runs = __popc(heads);
-  if (runs == 0) return;
+  if (live == 0u) return;
+  const unsigned same = __match_any_sync(0xffffffffu, id);       // every lane, before any condition
+  const unsigned heads = __ballot_sync(0xffffffffu, id >= 0 && lane == __ffs(same) - 1);   // an adapter's first row
+  const int adapters = __popc(heads);
   for (int k0 = 0; k0 < p.r; k0 += 64) {
     const int kn = p.r - k0 < 64 ? p.r - k0 : 64;
     __syncwarp();
@@ -624,26 +624,32 @@ __device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int6
             e < rows && c < kn ? *reinterpret_cast<const float4*>(p.T + (row0 + e) * p.r + k0 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     __syncwarp();
-    if (runs <= 2) {                           // the end of one run and the beginning of the next
-      const int h0 = __ffs(heads) - 1, h1 = runs > 1 ? 31 - __clz(heads) : kG;
-      const bf16* ga = p.G + __shfl_sync(0xffffffffu, id, h0) * p.strideG;
-      const bf16* gb = p.G + __shfl_sync(0xffffffffu, id, h1 < kG ? h1 : h0) * p.strideG;
-      const unsigned first = live & ((1u << h1) - 1u), second = live & ~((1u << h1) - 1u);
-      uint4 ua[2], ub[2];
-      load_g(p, ga, ff, k0, ua);
-      load_g(p, gb, ff, k0, ub);
-      for (int k1 = 0; k1 < kn; k1 += 16) {
-        uint4 na[2], nb[2];
-        const int kx = k1 + 16 < kn ? k0 + k1 + 16 : k0;
-        load_g(p, ga, ff, kx, na);
-        load_g(p, gb, ff, kx, nb);
+    if (adapters <= 4) {                       // the values of two adapters at a time, for all rows
+      unsigned left = heads;
+      while (left) {
+        const int h0 = __ffs(left) - 1;
+        left &= left - 1;
+        const int h1 = left ? __ffs(left) - 1 : h0;
+        if (left) left &= left - 1;
+        const int a0 = __shfl_sync(0xffffffffu, id, h0), a1 = __shfl_sync(0xffffffffu, id, h1);
+        const unsigned first = __ballot_sync(0xffffffffu, id == a0), second = __ballot_sync(0xffffffffu, id == a1);
+        const bf16 *ga = p.G + a0 * p.strideG, *gb = p.G + a1 * p.strideG;
+        uint4 ua[2], ub[2];
+        load_g(p, ga, ff, k0, ua);
+        load_g(p, gb, ff, k0, ub);
+        for (int k1 = 0; k1 < kn; k1 += 16) {
+          uint4 na[2], nb[2];
+          const int kx = k1 + 16 < kn ? k0 + k1 + 16 : k0;
+          load_g(p, ga, ff, kx, na);
+          load_g(p, gb, ff, kx, nb);
 #pragma unroll
-        for (int e = 0; e < kG; ++e) {
-          const float x = sum16(ua, Ts + e * 64 + k1), y = sum16(ub, Ts + e * 64 + k1);
-          v[e] += ((first >> e) & 1u) ? x : ((second >> e) & 1u) ? y : 0.f;
+          for (int e = 0; e < kG; ++e) {
+            const float x = sum16(ua, Ts + e * 64 + k1), y = sum16(ub, Ts + e * 64 + k1);
+            v[e] += ((first >> e) & 1u) ? x : ((second >> e) & 1u) ? y : 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) { ua[i] = na[i]; ub[i] = nb[i]; }
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) { ua[i] = na[i]; ub[i] = nb[i]; }
       }
     } else {                                   // an adapter a row, eight rows at a time
       for (int k1 = 0; k1 < kn; k1 += 16) {

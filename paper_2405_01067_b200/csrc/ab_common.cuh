@@ -172,6 +172,8 @@ struct SplitBatch { int count, tiles, bn; };
 SplitBatch gemm_split_plan(SplitGemm* probs, int count);      // fills first_tile; the table then goes to the device
 int gemm_split_batched(const SplitGemm* d_probs, const SplitBatch& b, int* status, cudaStream_t st);   // fp32 operands
 int gemm_split_one(SplitGemm p, bool src_bf16, int* status, cudaStream_t st);    // one problem; clears *status first
+constexpr int kSplitFew = 8;
+int gemm_split_few(SplitGemm* probs, int count, bool src_bf16, int* status, cudaStream_t st);   // up to kSplitFew, host table
 
 // Copies a host table to the device in pieces the runtime stages without waiting for the stream (a pageable copy of
 // more than 64 KB waits until the stream has drained), under stream capture as arguments of kernels: either way the table may go

@@ -511,6 +511,14 @@ gemm_split_one_kernel(const __grid_constant__ SplitGemm p, int ntiles, int* stat
   gemm_split_body<BN, kBf16, true>(&p, 1, ntiles, status);
 }
 
+// A few problems as kernel parameters, found by the finder warp.
+struct SplitFew { SplitGemm p[kSplitFew]; };
+template <int BN, bool kBf16>
+__global__ void __launch_bounds__(kThreads, 1)
+gemm_split_few_kernel(const __grid_constant__ SplitFew t, int nprobs, int ntiles, int* status) {
+  gemm_split_body<BN, kBf16, false>(t.p, nprobs, ntiles, status);
+}
+
 template <typename... KArgs, typename... Args>
 int launch(void (*kernel)(KArgs...), size_t smem, int tiles, cudaStream_t st, Args... args) {
   const int sms = sm_count();
@@ -571,6 +579,20 @@ int gemm_split_one(SplitGemm p, bool src_bf16, int* status, cudaStream_t st) {
   }
   if (b.bn == 128) return launch(gemm_split_one_kernel<128, false>, Cfg<128, false>::kSmem, b.tiles, st, p, b.tiles, status);
   return launch(gemm_split_one_kernel<64, false>, Cfg<64, false>::kSmem, b.tiles, st, p, b.tiles, status);
+}
+
+// The slices of a reduction, or other products that are few: one launch, nothing in device memory.  status is not cleared.
+int gemm_split_few(SplitGemm* probs, int count, bool src_bf16, int* status, cudaStream_t st) {
+  if (count < 1 || count > kSplitFew) return AB_ERR_INVALID_ARG;
+  const SplitBatch b = gemm_split_plan(probs, count);
+  SplitFew t = {};
+  for (int i = 0; i < count; ++i) t.p[i] = probs[i];
+  if (src_bf16) {
+    if (b.bn == 128) return launch(gemm_split_few_kernel<128, true>, Cfg<128, true>::kSmem, b.tiles, st, t, count, b.tiles, status);
+    return launch(gemm_split_few_kernel<64, true>, Cfg<64, true>::kSmem, b.tiles, st, t, count, b.tiles, status);
+  }
+  if (b.bn == 128) return launch(gemm_split_few_kernel<128, false>, Cfg<128, false>::kSmem, b.tiles, st, t, count, b.tiles, status);
+  return launch(gemm_split_few_kernel<64, false>, Cfg<64, false>::kSmem, b.tiles, st, t, count, b.tiles, status);
 }
 
 }  // namespace ab
