@@ -565,7 +565,7 @@ struct OutParams {
   const bf16* G; int64_t strideG;
   bf16* Out;
   int bn, nft, ntiles, ns, slot_bytes, tmem_cols;
-  int csize;                                // few_kernel: CTAs of a cluster
+  int csize, share, g_slots;                // few_kernel: CTAs of a cluster, rows that each finishes, pieces of G at a time
   int* status;
 };
 
@@ -911,30 +911,39 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
 }
 
 // ------------------------------------------------------------------------------------------------ the same for few rows
-// One tile of 128 features x all rows (bn, at most 128) a cluster; its CTAs have a part of the reduction each.  Their partial sums
-// meet in the shared memory of the CTA that finishes a share of the rows, which adds them in rank order.  The adapters' part of
-// those rows is summed by the epilogue warps while W is still arriving.
+// A tile of 128 features x bn rows a cluster; its CTAs have a part of the reduction each.  Their partial sums meet in the shared memory of
+// the CTA that finishes a share of the rows, which adds them in rank order.  The adapters' part goes row by row over the fp32 pipes: the
+// tile's piece of G_a is fetched (once for neighbouring rows of one adapter) while W is still arriving and T not yet there.
+// Loops are short and not unrolled: the code runs once, and fetching it is part of the latency.
 struct FewBars {
-  uint64_t full[kMaxStages], empty[kMaxStages], acc_full;
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full, g_full;
   uint32_t tmem_base;
   int abort_any;
 };
-constexpr int kFewRows = 128;
+constexpr int kBatch = 16;                // rows whose T and G are in shared memory at a time, at most
+
 __global__ void __launch_bounds__(kWideThreads, 1)
-few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const OutParams p) {
+few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ OutParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const int share = (p.bn + p.csize - 1) / p.csize;               // rows that a CTA finishes
-  float* red = reinterpret_cast<float*>(ring + (size_t)p.ns * p.slot_bytes);      // [csize][share][128]
-  float* tbuf = red + (size_t)p.csize * share * 128;              // T of 16 rows for each epilogue warp
-  FewBars* b = reinterpret_cast<FewBars*>(tbuf + 4 * kG * 64);
+  uint8_t* gbuf = ring + (size_t)p.ns * p.slot_bytes;                          // g_slots pieces of G: [128][r], or [r][128]
+  float* Tb = reinterpret_cast<float*>(gbuf + (size_t)p.g_slots * 256 * p.r);  // [kBatch][r]
+  float* dl = Tb + kBatch * p.r;                                               // [share][128]: the adapters' part of this CTA's rows
+  const int pitch = p.share + 4;
+  float* red = dl + p.share * 128;                                             // [csize][128][pitch]: partial sums of this CTA's rows
+  FewBars* b = reinterpret_cast<FewBars*>(red + (size_t)p.csize * 128 * pitch);
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int ft = (int)blockIdx.x / p.csize, rank = (int)blockIdx.x - ft * p.csize, f0 = ft * 128;
+  const int64_t row0 = (int64_t)blockIdx.y * p.bn;
+  const int rows = (int)(p.N - row0 < p.bn ? p.N - row0 : p.bn);
   const int per = (p.nk + p.csize - 1) / p.csize, i0 = rank * per, i1 = i0 + per < p.nk ? i0 + per : p.nk;
+  const int qw = warp & 3, fl = qw * 32 + lane, t0 = rank * p.share;
+  const int t1 = t0 + p.share < rows ? t0 + p.share : rows;                    // the rows that this CTA finishes
   dep_launch();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
     mbar_init(&b->acc_full, 1);
+    mbar_init(&b->g_full, 1);
     b->abort_any = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tmW); tma_prefetch_desc(&tmIn);
@@ -945,7 +954,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
-  float acc[kG];
+  bool ok = true;
 
   if (warp == 0) {
     int slot = 0, ph = 1;
@@ -957,7 +966,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
         mbar_arrive_expect_tx(bar, kABytes + p.bn * 128);
         if (p.mn) { tma_load_2d(dst, &tmW, bar, f0, i * 64); tma_load_2d(dst + 8192, &tmW, bar, f0 + 64, i * 64); }
         else tma_load_2d(dst, &tmW, bar, i * 64, f0);
-        tma_load_2d(dst + kABytes, &tmIn, bar, i * 64, 0);
+        tma_load_2d(dst + kABytes, &tmIn, bar, i * 64, (int)row0);
       }
       __syncwarp();
       if (++slot == p.ns) { slot = 0; ph ^= 1; }
@@ -983,27 +992,91 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
     }
     if (elect_one()) tc_commit(&b->acc_full);
     __syncwarp();
-  }
-  const int qw = warp & 3, f = f0 + qw * 32 + lane, t0 = rank * share;
-  const int t1 = t0 + share < p.N ? t0 + share : (int)p.N;        // the rows that this CTA finishes
-  bool ok = true;
-  if (warp >= 2) {
-    dep_wait();                            // T is complete
+  } else {
+    const int nf = p.P - f0 < 128 ? p.P - f0 : 128;          // features of the tile
+    bool waited = false;
+    for (int b0 = t0, turn = 0; b0 < t1;) {
+      // the batch: rows up to the one that would want a piece of G too many; a row's piece
+      const int id = lane < kBatch && b0 + lane < t1 ? clean_id(p.ids[row0 + b0 + lane], p.L) : -1;
+      const int before = __shfl_up_sync(0xffffffffu, id, 1);
+      const bool head = id >= 0 && (lane == 0 || id != before);
+      const unsigned heads = __ballot_sync(0xffffffffu, head);
+      const int piece = __popc(heads & (0xffffffffu >> (31 - lane))) - 1;
+      const unsigned over = __ballot_sync(0xffffffffu, head && piece == p.g_slots);
+      int n = t1 - b0 < kBatch ? t1 - b0 : kBatch;
+      if (over && __ffs(over) - 1 < n) n = __ffs(over) - 1;
+      const int pieces = __popc(heads & (n < 32 ? (1u << n) - 1u : 0xffffffffu));
+      if (warp == 2 && pieces > 0) {
+        if (lane == 0) mbar_arrive_expect_tx(&b->g_full, (uint32_t)(pieces * nf * p.r * 2));
+        __syncwarp();
+        unsigned left = heads;
+        for (int g = 0; g < pieces; ++g) {
+          const int e = __ffs(left) - 1;
+          left &= left - 1;
+          const bf16* G = p.G + __shfl_sync(0xffffffffu, id, e) * p.strideG;
+          uint8_t* dst = gbuf + (size_t)g * 256 * p.r;
+          if (!p.mn) {
+            if (lane == 0) bulk_load(dst, G + (int64_t)f0 * p.r, (uint32_t)(nf * p.r * 2), &b->g_full);
+          } else {
+            for (int k = lane; k < p.r; k += 32) bulk_load(dst + k * 256, G + (int64_t)k * p.P + f0, (uint32_t)(nf * 2), &b->g_full);
+          }
+        }
+        __syncwarp();
+      }
+      if (!waited) {
+        dep_wait();                        // T is complete; and this kernel is done only after the ones before it
+        waited = true;
+      }
+      const int rq = p.r / 4;
+      for (int i = threadIdx.x - 64; i < n * rq; i += 128) {
+        const int e = i / rq, c = i - e * rq;
+        *reinterpret_cast<float4*>(Tb + e * p.r + 4 * c) = *reinterpret_cast<const float4*>(p.T + (row0 + b0 + e) * p.r + 4 * c);
+      }
+      if (pieces > 0 && !mbar_wait_warp(&b->g_full, turn & 1)) { raise(&b->abort_any, p.status); ok = false; }
+      named_bar_sync(1, 128);
+      const int oct = p.r / 8, c0 = fl % oct;
+#pragma unroll 1
+      for (int e = 0; e < n; ++e) {
+        const int a = __shfl_sync(0xffffffffu, id, e), g = __shfl_sync(0xffffffffu, piece, e);
+        float s = 0.f;
+        if (a >= 0) {
+          const uint8_t* G = gbuf + (size_t)g * 256 * p.r;
+          const float* T = Tb + e * p.r;
+          if (!p.mn) {
+            // a lane begins at an eighth of its own: lanes a whole number of bank rows apart would meet in one bank
+            int c = c0;
+#pragma unroll 2
+            for (int i = 0; i < oct; ++i) {
+              const uint4 u = *reinterpret_cast<const uint4*>(G + fl * p.r * 2 + c * 16);
+              const float4 x = *reinterpret_cast<const float4*>(T + 8 * c), y = *reinterpret_cast<const float4*>(T + 8 * c + 4);
+              const float t[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+              dot8(u, t, s);
+              if (++c == oct) c = 0;
+            }
+          } else {
+#pragma unroll 8
+            for (int k = 0; k < p.r; ++k) s = fmaf(__bfloat162float(*reinterpret_cast<const bf16*>(G + k * 256 + fl * 2)), T[k], s);
+          }
+        }
+        dl[(b0 - t0 + e) * 128 + fl] = s;
+      }
+      named_bar_sync(1, 128);              // the pieces and T have been read
+      b0 += n;
+      turn += pieces > 0 ? 1 : 0;          // a batch without pieces does not use the barrier
+    }
+    if (!waited) dep_wait();
     if (ft == 0 && rank == 0 && warp == 2) {
       bool bad = false;
-      for (int t = lane; t < p.N; t += 32) bad |= p.ids[t] < -1 || p.ids[t] >= p.L;
+      for (int t = lane; t < rows; t += 32) bad |= p.ids[row0 + t] < -1 || p.ids[row0 + t] >= p.L;
       if (__any_sync(0xffffffffu, bad) && lane == 0) atomicExch(p.status, (int)AB_ERR_INVALID_ARG);
     }
-#pragma unroll
-    for (int e = 0; e < kG; ++e) acc[e] = 0.f;
-    if (t0 < t1 && f0 + qw * 32 < p.P) add_mixed(p, t0, t1, f, lane, tbuf + (warp - 2) * kG * 64, acc);
-    ok = mbar_wait_warp(&b->acc_full, 0);
-    if (!ok) raise(&b->abort_any, p.status);
+    if (!mbar_wait_warp(&b->acc_full, 0)) { raise(&b->abort_any, p.status); ok = false; }
   }
   cluster_wait();                          // every CTA of the cluster runs
   if (warp >= 2) {
     tc_fence_after();
-    const uint32_t dst = smem_u32(red) + (uint32_t)((rank * share * 128 + qw * 32 + lane) * 4);
+    const uint32_t dst = smem_u32(red) + (uint32_t)((rank * 128 + fl) * pitch * 4);
+#pragma unroll 1
     for (int c = 0; c < p.bn; c += kG) {
       float v[kG];
       if (ok && i1 > i0) tmem_ld16(tmem + ((uint32_t)(qw * 32) << 16) + c, v);
@@ -1012,30 +1085,28 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
         for (int e = 0; e < kG; ++e) v[e] = 0.f;
       }
 #pragma unroll
-      for (int e = 0; e < kG; ++e) {
-        const int t = c + e, owner = t / share;
-        const uint32_t to = cluster_addr(dst + (uint32_t)((t - owner * share) * 512), owner);
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v[e]) : "memory");
+      for (int e = 0; e < kG; e += 4) {    // a share is a multiple of four rows
+        const int owner = (c + e) / p.share;
+        const uint32_t to = cluster_addr(dst + (uint32_t)((c + e - owner * p.share) * 4), owner);
+        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(v[e]), "f"(v[e + 1]), "f"(v[e + 2]), "f"(v[e + 3]) : "memory");
       }
     }
     tc_fence_before();
   }
   cluster_arrive();
   cluster_wait();                          // and has written its sums
-  if (warp >= 2 && f0 + qw * 32 < p.P) {
-    for (int e0 = 0; t0 + e0 < t1; e0 += kG) {
-      if (e0 > 0) {
-#pragma unroll
-        for (int e = 0; e < kG; ++e) acc[e] = 0.f;
-        add_mixed(p, t0 + e0, t1, f, lane, tbuf + (warp - 2) * kG * 64, acc);
+  if (warp >= 2 && f0 + fl < p.P) {
+#pragma unroll 1
+    for (int t = t0; t < t1; t += 4) {
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int q = 0; q < p.csize; ++q) {
+        const float4 x = *reinterpret_cast<const float4*>(red + (q * 128 + fl) * pitch + t - t0);
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
       }
+      const float y[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int e = 0; e < kG; ++e) {
-        if (t0 + e0 + e >= t1 || f >= p.P) continue;
-        float v = 0.f;
-        for (int q = 0; q < p.csize; ++q) v += red[(q * share + e0 + e) * 128 + qw * 32 + lane];
-        p.Out[(int64_t)(t0 + e0 + e) * p.P + f] = __float2bfloat16_rn(v + acc[e]);
-      }
+      for (int e = 0; e < 4; ++e)
+        if (t + e < t1) p.Out[(row0 + t + e) * p.P + f0 + fl] = __float2bfloat16_rn(y[e] + dl[(t - t0 + e) * 128 + fl]);
     }
   }
   __syncthreads();
@@ -1267,14 +1338,24 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
 int pad16(int r) { return (r + 15) / 16 * 16; }
 int pow2_cols(int c) { int v = 32; while (v < c) v <<= 1; return v; }
 
+constexpr int kFewRows = 128;
+constexpr int kTbuf = 4 * kG * 64 * 4;
+
+// Whether few_kernel takes the rows: up to 128, and more while tiles of 64 rows leave an SM each for two CTAs of a cluster
+bool few_rows(int64_t N, int P) {
+  if (N <= kFewRows) return true;
+  const int sms = sm_count() > 0 ? sm_count() : 148;
+  return N <= 1024 && (N + 63) / 64 * ((P + 127) / 128) * 2 <= sms;
+}
+
 // the stride of a lone matrix may be anything
 int stack_map(CUtensorMap* m, const AdapterCall& c, const void* F, int rows, int cols, int64_t stride, int box_rows) {
   return make_tensor_map_stack(m, F, c.L, rows, cols, c.L > 1 ? stride : (int64_t)rows * cols, box_rows);
 }
 
 // T = s F In of all rows (two launches, or one for few rows); `first`: nothing of the call was launched before
-int launch_project(const AdapterCall& c, const void* In, int K, const void* F, int64_t strideF, bool f_mn, float* T, bool want_T, bf16* P, bool first,
-                   int* status) {
+int launch_project(const AdapterCall& c, const void* In, int K, const void* F, int64_t strideF, bool f_mn, float* T, bool want_T, int out_width, bf16* P,
+                   bool first, int* status) {
   const int sms = sm_count();
   if (sms <= 0) return AB_ERR_CUDA;
   ProjParams p;
@@ -1282,7 +1363,7 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   const int rp = pad16(c.r);
   p.In = static_cast<const bf16*>(In); p.N = c.N; p.K = K; p.F = static_cast<const bf16*>(F); p.strideF = strideF; p.f_mn = f_mn ? 1 : 0;
   p.scale = c.scale; p.ids = c.ids; p.T = T; p.P = P; p.r = c.r; p.rp = rp; p.L = c.L; p.first = first ? 1 : 0; p.status = status;
-  p.want_T = want_T || c.N <= kFewRows ? 1 : 0;
+  p.want_T = want_T || few_rows(c.N, out_width) ? 1 : 0;
   p.all_rows = c.N <= 64 ? 1 : 0;
   p.tile_rows = c.N > 1024 ? 128 : 64;
   const int64_t tiles = (c.N + p.tile_rows - 1) / p.tile_rows;
@@ -1329,8 +1410,6 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   return launch_after(project_tc_kernel<8>, grid, (unsigned)kProjTcThreads, smem, p.csize, c.st, tmIn, tmF, p);
 }
 
-constexpr int kTbuf = 4 * kG * 64 * 4;
-
 // Out = In W^T + T G^T; mn as in OutParams
 int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void* G, int64_t strideG, void* Out, int P, const float* T, const bf16* Tp,
                int* status) {
@@ -1345,20 +1424,26 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
   CUtensorMap tmW, tmIn, tmG, tmT, tmOut;
   if (mn) AB_TRY(make_tensor_map_2d(&tmW, c.W, false, K, P, P, 64, 64));
   else AB_TRY(make_tensor_map_2d(&tmW, c.W, false, P, K, K, 64, 128));
-  if (c.N <= kFewRows) {
-    p.bn = (int)((c.N + 15) / 16 * 16);
+  if (few_rows(c.N, P)) {
+    p.bn = c.N <= 64 ? (int)((c.N + 15) / 16 * 16) : 64;
+    const int64_t tt = (c.N + p.bn - 1) / p.bn;
     p.csize = 8;
-    while (p.csize > 1 && (p.nft * p.csize > sms || 2 * p.csize > p.nk)) p.csize >>= 1;
+    while (p.csize > 1 && (p.nft * tt * p.csize > sms || 2 * p.csize > p.nk)) p.csize >>= 1;
+    p.share = ((p.bn + p.csize - 1) / p.csize + 3) / 4 * 4;
     p.slot_bytes = kABytes + p.bn * 128;
-    const int share = (p.bn + p.csize - 1) / p.csize;
-    const size_t red = (size_t)p.csize * share * 512;
-    p.ns = (int)((kMaxSmem - 2048 - red - kTbuf - sizeof(FewBars)) / p.slot_bytes);
+    // 48 KB for G, as many pieces as a batch has rows at most; with 64 rows of rank 256 in one CTA's hands 146 KB beside the ring
+    const size_t piece = (size_t)256 * c.r;
+    p.g_slots = (int)(49152 / piece < kBatch ? 49152 / piece : kBatch);
+    if (p.g_slots < 1) p.g_slots = 1;
+    if (p.g_slots > p.share) p.g_slots = p.share;
+    const size_t rest = p.g_slots * piece + (size_t)kBatch * c.r * 4 + (size_t)p.share * 512 + (size_t)p.csize * 128 * (p.share + 4) * 4 + sizeof(FewBars);
+    p.ns = (int)((kMaxSmem - 2048 - rest) / p.slot_bytes);
     if (p.ns > kMaxStages) p.ns = kMaxStages;
     p.tmem_cols = pow2_cols(p.bn);
     AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn));
     AB_CUDA_OK(allow_smem(few_kernel));
-    return launch_after(few_kernel, (unsigned)(p.nft * p.csize), (unsigned)kWideThreads, 1024 + (size_t)p.ns * p.slot_bytes + red + kTbuf + sizeof(FewBars),
-                        p.csize, c.st, tmW, tmIn, p);
+    return launch_after(few_kernel, dim3((unsigned)(p.nft * p.csize), (unsigned)tt), (unsigned)kWideThreads,
+                        1024 + (size_t)p.ns * p.slot_bytes + rest, p.csize, c.st, tmW, tmIn, p);
   }
   // rows of a tile: cycles of the busiest SM, a slab's operands arriving at 64 bytes a cycle or its MMAs, whichever is longer
   double best = 1e30;
@@ -1480,7 +1565,7 @@ size_t adapter_tc_ws(int64_t N, int m, int n, int r, int L) { return tc_ws(nullp
 int adapter_tc_forward(const AdapterCall& c, void* y, float* T_save, void* ws) {
   const TcWs w = tc_ws(ws, c.N, c.m, c.n, c.r, c.L);
   float* T = T_save ? T_save : w.T;
-  AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, T, T_save != nullptr, w.TP, true, w.status));
+  AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, T, T_save != nullptr, c.m, w.TP, true, w.status));
   return launch_out(c, c.x, c.n, false, c.A, c.strideA, y, c.m, T, w.TP, w.status);
 }
 
@@ -1488,11 +1573,11 @@ int adapter_tc_backward(const AdapterCall& c, const void* dY, const float* T_sav
   const TcWs w = tc_ws(ws, c.N, c.m, c.n, c.r, c.L);
   bool first = true;
   if (dX || dB) {
-    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, false, w.UP, first, w.status));
+    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, false, c.n, w.UP, first, w.status));
     first = false;
   }
   if (dA && !T_saved) {
-    AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, false, w.TP, first, w.status));
+    AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, false, c.m, w.TP, first, w.status));
     first = false;
   }
   if (dX) AB_TRY(launch_out(c, dY, c.m, true, c.B, c.strideB, dX, c.n, w.U, w.UP, w.status));
