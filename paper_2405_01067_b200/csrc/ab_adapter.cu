@@ -126,13 +126,15 @@ project_kernel(const TI* __restrict__ In, const TI* __restrict__ F, int64_t stri
 
 // out[i][c] = sum over the slices of base + sum_k T[i][k] G_a(c, k), rounded once; G_a(c, k) at G + a strideG + c g_c + k g_k.  base may be
 // out itself (fp32, one slice).  A map entry that is neither an adapter nor -1 is reported.  A thread has a column and kRD rows; sixteen
-// of G's values at a time are in registers, and stay there while the next row has the same adapter.
+// of G's values at a time are in registers, and stay there while the next row has the same adapter.  Where G_a's rows run along k
+// (g_k 1), they come by way of shared memory: read by column, a warp's load would touch 32 lines.
 constexpr int kDeltaCols = 256, kDeltaK = 64;
 template <typename TI, typename TO, int kRD>
 __global__ void __launch_bounds__(kDeltaCols)
 delta_kernel(const float* base, int slices, const float* __restrict__ T, const TI* __restrict__ G, int64_t strideG, int64_t g_c, int64_t g_k,
              const int* __restrict__ ids, TO* out, int64_t N, int P, int r, int L, int* status) {
   __shared__ float Ts[kRD][kDeltaK];
+  __shared__ float Gs[kDeltaCols][17];
   __shared__ int id[kRD];
   tc::dep_wait();
   tc::dep_launch();
@@ -161,9 +163,23 @@ delta_kernel(const float* base, int slices, const float* __restrict__ T, const T
         if (i >= rows || id[i] < 0) continue;
         if (id[i] != have) {
           have = id[i];
-          const TI* q = G + have * strideG + cc * g_c + (k0 + k1) * g_k;
+          if (g_k == 1) {
+            const TI* q = G + have * strideG + k0 + k1;
+            const int c0 = blockIdx.y * kDeltaCols, e = threadIdx.x & 15;
+            __syncthreads();
 #pragma unroll
-          for (int e = 0; e < 16; ++e) g[e] = k1 + e < kn ? to_f32(q[e * g_k]) : 0.f;
+            for (int u = 0; u < kDeltaCols / 16; ++u) {
+              const int col = u * 16 + (threadIdx.x >> 4);
+              Gs[col][e] = c0 + col < P && k1 + e < kn ? to_f32(q[(c0 + col) * g_c + e]) : 0.f;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i2 = 0; i2 < 16; ++i2) g[i2] = Gs[threadIdx.x][i2];
+          } else {
+            const TI* q = G + have * strideG + cc * g_c + (k0 + k1) * g_k;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) g[e] = k1 + e < kn ? to_f32(q[e * g_k]) : 0.f;
+          }
         }
         float v = acc[i];
 #pragma unroll
@@ -237,9 +253,9 @@ list_rows_kernel(const int* __restrict__ ids, int64_t N, int L, int* __restrict_
 }
 
 // D_a(f, k) = sum over the rows i of adapter a of In[i][f] S[i][k], at D + a strideD + f d_f + k d_k, for one or two such gradients.  A block
-// has 64 values of f and 32 of k of one adapter; rows in their order, 32 at a time in fp32, those sums in fp64: a long sum loses
+// has 64 values of f and 32 of k of one adapter; rows in their order, 64 at a time in fp32, those sums in fp64: a long sum loses
 // nothing that fp32 shows.
-constexpr int kGF = 64, kGK = 32, kGR = 32;
+constexpr int kGF = 64, kGK = 32, kGR = 64;
 struct GradSide { const void* In; int P, tiles; const float* S; float* D; int64_t strideD, d_f, d_k; };
 struct GradSides { GradSide side[2]; };
 template <typename TI>

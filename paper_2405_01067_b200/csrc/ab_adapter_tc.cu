@@ -233,13 +233,13 @@ __device__ __forceinline__ void rows_body(const ProjParams& p, int64_t unit, int
           float v = 0.f;
           if (k < p.r) {
             const uint4* f = reinterpret_cast<const uint4*>(p.F + a * p.strideF + (int64_t)k * p.K);
-            for (int j = lane; j < p.K / 8; j += 128) {
-              uint4 u[4], w[4];
+            for (int j = lane; j < p.K / 8; j += 256) {
+              uint4 u[8], w[8];
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
+              for (int e = 0; e < 8; ++e)
                 if (j + 32 * e < p.K / 8) { u[e] = f[j + 32 * e]; w[e] = x[j + 32 * e]; }
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
+              for (int e = 0; e < 8; ++e)
                 if (j + 32 * e < p.K / 8) {
                   const uint32_t xs[4] = {w[e].x, w[e].y, w[e].z, w[e].w};
                   float t[8];
@@ -1034,31 +1034,46 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
       }
       if (pieces > 0 && !mbar_wait_warp(&b->g_full, turn & 1)) { raise(&b->abort_any, p.status); ok = false; }
       named_bar_sync(1, 128);
+      // four rows at a time, whose sums hide each other's latency; a row without an adapter is summed with whatever lies there, and
+      // gets 0
       const int oct = p.r / 8, c0 = fl % oct;
 #pragma unroll 1
-      for (int e = 0; e < n; ++e) {
-        const int a = __shfl_sync(0xffffffffu, id, e), g = __shfl_sync(0xffffffffu, piece, e);
-        float s = 0.f;
-        if (a >= 0) {
-          const uint8_t* G = gbuf + (size_t)g * 256 * p.r;
-          const float* T = Tb + e * p.r;
-          if (!p.mn) {
-            // a lane begins at an eighth of its own: lanes a whole number of bank rows apart would meet in one bank
-            int c = c0;
-#pragma unroll 2
-            for (int i = 0; i < oct; ++i) {
-              const uint4 u = *reinterpret_cast<const uint4*>(G + fl * p.r * 2 + c * 16);
-              const float4 x = *reinterpret_cast<const float4*>(T + 8 * c), y = *reinterpret_cast<const float4*>(T + 8 * c + 4);
-              const float t[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-              dot8(u, t, s);
-              if (++c == oct) c = 0;
-            }
-          } else {
-#pragma unroll 8
-            for (int k = 0; k < p.r; ++k) s = fmaf(__bfloat162float(*reinterpret_cast<const bf16*>(G + k * 256 + fl * 2)), T[k], s);
-          }
+      for (int e0 = 0; e0 < n; e0 += 4) {
+        const uint8_t* G[4];
+        const float* T[4];
+        float s[4];
+        unsigned has = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int a = __shfl_sync(0xffffffffu, id, e0 + e), g = __shfl_sync(0xffffffffu, piece, e0 + e);
+          has |= a >= 0 && e0 + e < n ? 1u << e : 0u;
+          G[e] = gbuf + (size_t)(a >= 0 && e0 + e < n ? g : 0) * 256 * p.r + (p.mn ? fl * 2 : fl * p.r * 2);
+          T[e] = Tb + (e0 + e) * p.r;
+          s[e] = 0.f;
         }
-        dl[(b0 - t0 + e) * 128 + fl] = s;
+        if (!p.mn) {
+          // a lane begins at an eighth of its own: lanes a whole number of bank rows apart would meet in one bank
+          int c = c0;
+#pragma unroll 1
+          for (int i = 0; i < oct; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint4 u = *reinterpret_cast<const uint4*>(G[e] + c * 16);
+              const float4 x = *reinterpret_cast<const float4*>(T[e] + 8 * c), y = *reinterpret_cast<const float4*>(T[e] + 8 * c + 4);
+              const float t[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+              dot8(u, t, s[e]);
+            }
+            if (++c == oct) c = 0;
+          }
+        } else {
+#pragma unroll 4
+          for (int k = 0; k < p.r; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = fmaf(__bfloat162float(*reinterpret_cast<const bf16*>(G[e] + k * 256)), T[e][k], s[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e0 + e < n) dl[(b0 - t0 + e0 + e) * 128 + fl] = ((has >> e) & 1u) ? s[e] : 0.f;
       }
       named_bar_sync(1, 128);              // the pieces and T have been read
       b0 += n;
@@ -1076,6 +1091,8 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
   if (warp >= 2) {
     tc_fence_after();
     const uint32_t dst = smem_u32(red) + (uint32_t)((rank * 128 + fl) * pitch * 4);
+    int owner = 0, at = 0;
+    uint32_t to = cluster_addr(dst, 0);
 #pragma unroll 1
     for (int c = 0; c < p.bn; c += kG) {
       float v[kG];
@@ -1086,9 +1103,11 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
       }
 #pragma unroll
       for (int e = 0; e < kG; e += 4) {    // a share is a multiple of four rows
-        const int owner = (c + e) / p.share;
-        const uint32_t to = cluster_addr(dst + (uint32_t)((c + e - owner * p.share) * 4), owner);
-        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(v[e]), "f"(v[e + 1]), "f"(v[e + 2]), "f"(v[e + 3]) : "memory");
+        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)at * 4), "f"(v[e]), "f"(v[e + 1]), "f"(v[e + 2]),
+                     "f"(v[e + 3])
+                     : "memory");
+        at += 4;
+        if (at == p.share && c + e + 4 < p.bn) { at = 0; to = cluster_addr(dst, ++owner); }
       }
     }
     tc_fence_before();
@@ -1096,17 +1115,20 @@ few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUte
   cluster_arrive();
   cluster_wait();                          // and has written its sums
   if (warp >= 2 && f0 + fl < p.P) {
-#pragma unroll 1
-    for (int t = t0; t < t1; t += 4) {
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int q = 0; q < p.csize; ++q) {
-        const float4 x = *reinterpret_cast<const float4*>(red + (q * 128 + fl) * pitch + t - t0);
+    bf16* out = p.Out + (row0 + t0) * p.P + f0 + fl;
+    const float* r0 = red + fl * pitch;
+#pragma unroll 2
+    for (int t = 0; t < t1 - t0; t += 4) {
+      float4 v = *reinterpret_cast<const float4*>(r0 + t);
+#pragma unroll 3
+      for (int q = 1; q < p.csize; ++q) {
+        const float4 x = *reinterpret_cast<const float4*>(r0 + q * 128 * pitch + t);
         v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
       }
       const float y[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (t + e < t1) p.Out[(row0 + t + e) * p.P + f0 + fl] = __float2bfloat16_rn(y[e] + dl[(t - t0 + e) * 128 + fl]);
+      for (int e = 0; e < 4; ++e, out += p.P)
+        if (t0 + t + e < t1) *out = __float2bfloat16_rn(y[e] + dl[(t + e) * 128 + fl]);
     }
   }
   __syncthreads();
@@ -1388,7 +1410,7 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   while (p.csize > 1 && (tiles * p.csize > 2 * sms || 2 * p.csize > p.nk)) p.csize >>= 1;
   // Up to three CTAs an SM, and no more room than for as many as there are: CTAs fill an SM before they go to the next.  The ring takes the
   // parts at the end.
-  const int64_t each = (tiles * p.csize * ((rp + 127) / 128) + sms - 1) / sms;
+  const int64_t each = (tiles * p.csize * ((rp + 127) / 128) + (c.N <= 2048 ? units : 0) + sms - 1) / sms;
   const int parts = p.tile_rows * (cols + 4) * 4, budget = each <= 1 ? 120 * 1024 : each == 2 ? 96 * 1024 : 72 * 1024;
   p.ns = budget / p.slot_bytes < 3 ? 3 : budget / p.slot_bytes < kMaxStages ? budget / p.slot_bytes : kMaxStages;
   if (p.ns * p.slot_bytes < parts) p.ns = (parts + p.slot_bytes - 1) / p.slot_bytes;
@@ -1431,9 +1453,10 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
     while (p.csize > 1 && (p.nft * tt * p.csize > sms || 2 * p.csize > p.nk)) p.csize >>= 1;
     p.share = ((p.bn + p.csize - 1) / p.csize + 3) / 4 * 4;
     p.slot_bytes = kABytes + p.bn * 128;
-    // 48 KB for G, as many pieces as a batch has rows at most; with 64 rows of rank 256 in one CTA's hands 146 KB beside the ring
+    // Up to 96 KB for G where a batch of rows with an adapter each then fits, else 48 KB; with 64 rows of rank 256 in one CTA's hands
+    // there are 146 KB beside the ring
     const size_t piece = (size_t)256 * c.r;
-    p.g_slots = (int)(49152 / piece < kBatch ? 49152 / piece : kBatch);
+    p.g_slots = piece * kBatch <= 98304 ? kBatch : (int)(49152 / piece);
     if (p.g_slots < 1) p.g_slots = 1;
     if (p.g_slots > p.share) p.g_slots = p.share;
     const size_t rest = p.g_slots * piece + (size_t)kBatch * c.r * 4 + (size_t)p.share * 512 + (size_t)p.csize * 128 * (p.share + 4) * 4 + sizeof(FewBars);
