@@ -452,7 +452,8 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
       const int g0 = (int)__shfl_sync(0xffffffffu, a, lane & 16);
       const unsigned same = __ballot_sync(0xffffffffu, a == g0 || !live);
       const bool mixed = ((same >> (lane & 16)) & 0xffffu) != 0xffffu;
-      b->row_ad[lrow] = !live || (mixed && !b->whole) ? -2 : p.want_T || mixed ? (a < 0 ? 0x7fffffff : a | 0x40000000) : a;
+      const bool mixed32 = same != 0xffffffffu || (int)__shfl_sync(0xffffffffu, a, 0) != (int)__shfl_sync(0xffffffffu, a, 16);
+      b->row_ad[lrow] = !live || (mixed && !b->whole) ? -2 : p.want_T || mixed32 ? (a < 0 ? 0x7fffffff : a | 0x40000000) : a;
     }
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
@@ -680,8 +681,8 @@ struct WideBars {
   int abort_any;
 };
 
-// The slabs of a tile behind the shared product's: for every run of groups with one adapter, piece by piece.  body(a, g0, g1, piece, j)
-// returns false to stop.
+// The slabs of a tile behind the shared product's: for every run of groups (lane l: group l's adapter) with one adapter, piece by piece.
+// body(a, g0, g1, piece, j) returns false to stop.
 template <typename F>
 __device__ __forceinline__ bool for_runs(int gid, int ngroups, int rp, F&& body) {
   int g = 0;
@@ -698,64 +699,91 @@ __device__ __forceinline__ bool for_runs(int gid, int ngroups, int rp, F&& body)
   return true;
 }
 
+// kPair: two CTAs have a tile of 256 features x bn rows together, 128 features each, and load half of the rows each: 32 KB a slab and
+// CTA instead of 48, which arrive as fast as they are multiplied (512 cycles against 520; alone 768).  An MMA's columns then come in
+// 32s, and so do the groups.
+template <bool kPair>
 __global__ void __launch_bounds__(kWideThreads, 1)
 wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmG,
-            const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmOut, const OutParams p) {
+            const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ OutParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* stg = ring + (size_t)p.ns * p.slot_bytes;              // per epilogue warp two tiles of 32 rows x 32 features
   float* tbuf = reinterpret_cast<float*>(stg + 4 * 2 * 2048);     // and T of 16 rows
   WideBars* b = reinterpret_cast<WideBars*>(tbuf + 4 * kG * 64);
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  constexpr int kCtas = kPair ? 2 : 1, kGroup = kG * kCtas;       // rows of a group
+  const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
+  const int first_tile = (int)blockIdx.x / kCtas, tile_step = (int)gridDim.x / kCtas;
+  const int half = p.bn / kCtas;                                  // rows that this CTA loads
   dep_launch();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&b->acc_full[i], 1); mbar_init(&b->acc_empty[i], 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&b->acc_full[i], 1); mbar_init(&b->acc_empty[i], 4 * kCtas); }
     b->abort_any = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tmW); tma_prefetch_desc(&tmIn); tma_prefetch_desc(&tmG); tma_prefetch_desc(&tmT); tma_prefetch_desc(&tmOut);
   }
-  if (warp == 1) tmem_alloc(&b->tmem_base, p.tmem_cols);
+  if (warp == 1) {
+    if constexpr (kPair) tmem_alloc_pair(&b->tmem_base, p.tmem_cols); else tmem_alloc(&b->tmem_base, p.tmem_cols);
+  }
   tc_fence_before();
   __syncthreads();
+  if constexpr (kPair) { cluster_arrive(); cluster_wait(); }      // the other CTA's barriers are there
   tc_fence_after();
   const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
-  const int ngroups = p.bn / kG;
+  const int ngroups = p.bn / kGroup;
+  // lane g: the adapter of group g, -1 none, -2 mixed
+  auto groups = [&](int row0, bool& bad) {
+    int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+    if constexpr (kPair) {
+      const int x = __shfl_sync(0xffffffffu, gid, (2 * lane) & 31), y = __shfl_sync(0xffffffffu, gid, (2 * lane + 1) & 31);
+      // a second half behind the last row goes with the first
+      gid = x == y || (int64_t)row0 + lane * kGroup + kG >= p.N ? x : -2;
+    }
+    return gid;
+  };
   // The kernels before this one started only after all that a caller had in the stream before: x, W, the factors and the map are
   // complete.  T alone comes from them, and is waited for where it is read.
 
   if (warp == 0) {
     int slot = 0, ph = 1;
     bool ok = true, waited = false;
-    const uint32_t tx = kABytes + p.bn * 128;
-    for (int tile = blockIdx.x; tile < p.ntiles && ok; tile += gridDim.x) {
-      const int f0 = (tile % p.nft) * 128, row0 = (tile / p.nft) * p.bn;
+    const uint32_t tx = kCtas * (kABytes + half * 128);
+    const uint32_t full0 = kPair ? cluster_addr(smem_u32(&b->full[0]), 0) : 0u;      // the first CTA's barriers count both CTAs' bytes
+    auto load_2d = [&](uint8_t* dst, const CUtensorMap* m, int s, int c0, int c1) {
+      if constexpr (kPair) tma_load_2d_pair(dst, m, full0 + (uint32_t)s * 8, c0, c1); else tma_load_2d(dst, m, &b->full[s], c0, c1);
+    };
+    auto load_3d = [&](uint8_t* dst, const CUtensorMap* m, int s, int c0, int c1, int c2) {
+      if constexpr (kPair) tma_load_3d_pair(dst, m, full0 + (uint32_t)s * 8, c0, c1, c2); else tma_load_3d(dst, m, &b->full[s], c0, c1, c2);
+    };
+    for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step) {
+      const int f0 = ((tile % p.nft) * kCtas + rank) * 128, row0 = (tile / p.nft) * p.bn;
       bool bad;
-      const int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+      const int gid = groups(row0, bad);
       for (int i = 0; i < p.nk; ++i) {
         if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
         if (elect_one()) {
           uint8_t* dst = ring + (size_t)slot * p.slot_bytes;
-          uint64_t* bar = &b->full[slot];
-          mbar_arrive_expect_tx(bar, tx);
-          if (p.mn) { tma_load_2d(dst, &tmW, bar, f0, i * 64); tma_load_2d(dst + 8192, &tmW, bar, f0 + 64, i * 64); }
-          else tma_load_2d(dst, &tmW, bar, i * 64, f0);
-          tma_load_2d(dst + kABytes, &tmIn, bar, i * 64, row0);
+          if (rank == 0) mbar_arrive_expect_tx(&b->full[slot], tx);
+          if (p.mn) { load_2d(dst, &tmW, slot, f0, i * 64); load_2d(dst + 8192, &tmW, slot, f0 + 64, i * 64); }
+          else load_2d(dst, &tmW, slot, i * 64, f0);
+          load_2d(dst + kABytes, &tmIn, slot, i * 64, row0 + rank * half);
         }
         __syncwarp();
         if (++slot == p.ns) { slot = 0; ph ^= 1; }
       }
       if (!ok) break;
       if (!waited) { dep_wait(); fence_proxy_async_all(); waited = true; }
-      ok = for_runs(gid, ngroups, p.rp, [&](int a, int, int, int piece, int j) {
+      ok = for_runs(gid, ngroups, p.rp, [&](int a, int g0, int g1, int piece, int j) {
         if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); return false; }
         if (elect_one()) {
           uint8_t* dst = ring + (size_t)slot * p.slot_bytes;
-          uint64_t* bar = &b->full[slot];
-          mbar_arrive_expect_tx(bar, tx);
-          if (p.mn) { tma_load_3d(dst, &tmG, bar, f0, j * 64, a); tma_load_3d(dst + 8192, &tmG, bar, f0 + 64, j * 64, a); }
-          else tma_load_3d(dst, &tmG, bar, j * 64, f0, a);
-          tma_load_2d(dst + kABytes, &tmT, bar, piece * p.rp + j * 64, row0);
+          if (rank == 0) mbar_arrive_expect_tx(&b->full[slot], tx);
+          if (p.mn) { load_3d(dst, &tmG, slot, f0, j * 64, a); load_3d(dst + 8192, &tmG, slot, f0 + 64, j * 64, a); }
+          else load_3d(dst, &tmG, slot, j * 64, f0, a);
+          // alone: all rows of the tile; a pair: each its half of the run's rows, at the head of the slot
+          load_2d(dst + kABytes, &tmT, slot, piece * p.rp + j * 64, kPair ? row0 + g0 * kGroup + rank * (g1 - g0) * kG : row0);
         }
         __syncwarp();
         if (++slot == p.ns) { slot = 0; ph ^= 1; }
@@ -763,77 +791,92 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       });
     }
   } else if (warp == 1) {
-    int slot = 0, ph = 0, it = 0;
-    bool ok = true;
-    const uint32_t base = uniform(smem_u32(ring)), idesc = instr_desc_bf16(128, p.bn, p.mn, 0);
-    const uint64_t dA = smem_desc_sw128(base, p.mn ? 8192 : 16), dB = smem_desc_sw128(base + kABytes, 16);
-    const uint64_t a_step = p.mn ? 128u : 2u, slot_step = (uint64_t)(p.slot_bytes >> 4);
-    for (int tile = blockIdx.x; tile < p.ntiles && ok; tile += gridDim.x, ++it) {
-      const int row0 = (tile / p.nft) * p.bn, buf = it & 1;
-      bool bad;
-      const int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad);
-      if (!mbar_wait_warp(&b->acc_empty[buf], ((it >> 1) & 1) ^ 1)) { raise(&b->abort_any, p.status); break; }
-      tc_fence_after();
-      const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1));
-      for (int i = 0; i < p.nk; ++i) {
-        if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
+    if (rank == 0) {
+      int slot = 0, ph = 0, it = 0;
+      bool ok = true;
+      const uint32_t base = uniform(smem_u32(ring)), idesc = instr_desc_bf16(128 * kCtas, p.bn, p.mn, 0);
+      const uint64_t dA = smem_desc_sw128(base, p.mn ? 8192 : 16), dB = smem_desc_sw128(base + kABytes, 16);
+      const uint64_t a_step = p.mn ? 128u : 2u, slot_step = (uint64_t)(p.slot_bytes >> 4);
+      auto mma = [&](uint32_t d, uint64_t da, uint64_t db, uint32_t id, uint32_t acc) {
+        if constexpr (kPair) tc_mma_bf16_pair(d, da, db, id, acc); else tc_mma_bf16(d, da, db, id, acc);
+      };
+      auto commit = [&](uint64_t* bar) {
+        if constexpr (kPair) tc_commit_pair(bar); else tc_commit(bar);
+      };
+      for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step, ++it) {
+        const int row0 = (tile / p.nft) * p.bn, buf = it & 1;
+        bool bad;
+        const int gid = groups(row0, bad);
+        if (!mbar_wait_warp(&b->acc_empty[buf], ((it >> 1) & 1) ^ 1)) { raise(&b->abort_any, p.status); break; }
         tc_fence_after();
-        const uint64_t da = dA + slot_step * slot, db = dB + slot_step * slot;
-        const int ksteps = (p.K - i * 64 + 15) >> 4;
-        if (elect_one()) {
+        const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1));
+        for (int i = 0; i < p.nk; ++i) {
+          if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
+          tc_fence_after();
+          const uint64_t da = dA + slot_step * slot, db = dB + slot_step * slot;
+          const int ksteps = (p.K - i * 64 + 15) >> 4;
+          if (elect_one()) {
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            if (kk < ksteps) tc_mma_bf16(tacc, da + a_step * kk, db + 2 * kk, idesc, (i | kk) != 0);
-          tc_commit(&b->empty[slot]);
+            for (int kk = 0; kk < 4; ++kk)
+              if (kk < ksteps) mma(tacc, da + a_step * kk, db + 2 * kk, idesc, (i | kk) != 0);
+            commit(&b->empty[slot]);
+          }
+          __syncwarp();
+          if (++slot == p.ns) { slot = 0; ph ^= 1; }
         }
+        if (!ok) break;
+        ok = for_runs(gid, ngroups, p.rp, [&](int, int g0, int g1, int, int j) {
+          if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); return false; }
+          tc_fence_after();
+          const uint64_t da = dA + slot_step * slot, db = dB + slot_step * slot + (uint64_t)(kPair ? 0 : g0 * (kG * 128 >> 4));
+          const uint32_t id = instr_desc_bf16(128 * kCtas, (g1 - g0) * kGroup, p.mn, 0);
+          const int ksteps = (p.rp - j * 64 + 15) >> 4;
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              if (kk < ksteps) mma(tacc + g0 * kGroup, da + a_step * kk, db + 2 * kk, id, 1u);
+            commit(&b->empty[slot]);
+          }
+          __syncwarp();
+          if (++slot == p.ns) { slot = 0; ph ^= 1; }
+          return true;
+        });
+        if (ok && elect_one()) commit(&b->acc_full[buf]);
         __syncwarp();
-        if (++slot == p.ns) { slot = 0; ph ^= 1; }
       }
-      if (!ok) break;
-      ok = for_runs(gid, ngroups, p.rp, [&](int, int g0, int g1, int, int j) {
-        if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); return false; }
-        tc_fence_after();
-        const uint64_t da = dA + slot_step * slot, db = dB + slot_step * slot + (uint64_t)(g0 * (kG * 128 >> 4));
-        const uint32_t id = instr_desc_bf16(128, (g1 - g0) * kG, p.mn, 0);
-        const int ksteps = (p.rp - j * 64 + 15) >> 4;
-        if (elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            if (kk < ksteps) tc_mma_bf16(tacc + g0 * kG, da + a_step * kk, db + 2 * kk, id, 1u);
-          tc_commit(&b->empty[slot]);
-        }
-        __syncwarp();
-        if (++slot == p.ns) { slot = 0; ph ^= 1; }
-        return true;
-      });
-      if (ok && elect_one()) tc_commit(&b->acc_full[buf]);
-      __syncwarp();
     }
   } else {
     const int qw = warp & 3;
     const uint32_t lane_base = (uint32_t)(qw * 32) << 16;
     uint8_t* my = stg + (size_t)(warp - 2) * 2 * 2048;
+    const uint32_t acc_empty0 = kPair ? cluster_addr(smem_u32(&b->acc_empty[0]), 0) : 0u;
+    auto give_back = [&](int buf) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (kPair) mbar_arrive_cluster(acc_empty0 + (uint32_t)buf * 8); else mbar_arrive(&b->acc_empty[buf]);
+      }
+    };
     int nst = 0, it = 0;
     bool ok = true;
     dep_wait();                          // T is complete; and this kernel is done only after the ones before it
-    for (int tile = blockIdx.x; tile < p.ntiles && ok; tile += gridDim.x, ++it) {
-      const int f0 = (tile % p.nft) * 128 + qw * 32, row0 = (tile / p.nft) * p.bn, buf = it & 1;
+    for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step, ++it) {
+      const int ftile = (tile % p.nft) * kCtas + rank, f0 = ftile * 128 + qw * 32, row0 = (tile / p.nft) * p.bn, buf = it & 1;
       bool bad;
-      const int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad);
-      if (tile % p.nft == 0 && qw == 0 && __any_sync(0xffffffffu, bad && lane * 8 < p.bn) && lane == 0) atomicExch(p.status, (int)AB_ERR_INVALID_ARG);
-      const unsigned mixed = __ballot_sync(0xffffffffu, gid == -2 && lane < ngroups);
+      const int gid = groups(row0, bad);
+      const bool any_bad = __any_sync(0xffffffffu, bad && lane * 8 < p.bn);
+      if (ftile == 0 && qw == 0 && any_bad && lane == 0) atomicExch(p.status, (int)AB_ERR_INVALID_ARG);
+      // bit g: the adapters' part of the 16 rows from 16 g goes over the fp32 pipes
+      unsigned mixed = __ballot_sync(0xffffffffu, __shfl_sync(0xffffffffu, gid, lane / kCtas) == -2 && lane < p.bn / kG);
       ok = mbar_wait_warp(&b->acc_full[buf], (it >> 1) & 1);
       if (!ok) { raise(&b->abort_any, p.status); break; }
       tc_fence_after();
       const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1)) + lane_base;
       const bool live = f0 < p.P;
-      for (int g0 = 0; g0 < ngroups; g0 += 2) {
+      const int n16 = p.bn / kG;
+      for (int g0 = 0; g0 < n16; g0 += 2) {
         if (!live || (int64_t)row0 + g0 * kG >= p.N) {
-          if (g0 + 2 >= ngroups) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&b->acc_empty[buf]);
-          }
+          if (g0 + 2 >= n16) give_back(buf);
           continue;
         }
         uint8_t* tile_s = my + (nst & 1) * 2048;
@@ -850,11 +893,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           tmem_ld16_nowait(tacc + g0 * kG + kG, v[1]);
         }
         tmem_wait_ld();
-        if (g0 + 2 >= ngroups) {         // the last columns are in registers: hand the accumulator back
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&b->acc_empty[buf]);
-        }
+        if (g0 + 2 >= n16) give_back(buf);         // the last columns are in registers
         if (!simt) {
           // eight rows (columns 8 j ..) of 32 features are four fragments; transposed they are 8 rows of 64 bytes, whose 16-byte pieces
           // lie where the swizzle puts them
@@ -876,7 +915,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
             float d[kG];
 #pragma unroll
             for (int e = 0; e < kG; ++e) d[e] = __uint_as_float(v[h][e]);
-            if ((mixed >> (g0 + h)) & 1u)
+            if (((mixed >> (g0 + h)) & 1u) && (int64_t)row0 + (g0 + h) * kG < p.N)
               add_mixed(p, (int64_t)row0 + (g0 + h) * kG, p.N, f0 + lane, lane, tbuf + (warp - 2) * kG * 64, d);
 #pragma unroll
             for (int e = 0; e < kG; ++e) {
@@ -904,10 +943,12 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     while (globaltimer_ns() - t0 < 200000ull) { }
     __syncthreads();
   }
+  if constexpr (kPair) { cluster_arrive(); cluster_wait(); }      // nothing of the other CTA's is on its way to this one's barriers
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, p.tmem_cols);
+    if constexpr (kPair) tmem_dealloc_pair(tmem, p.tmem_cols); else tmem_dealloc(tmem, p.tmem_cols);
   }
+  if constexpr (kPair) { cluster_arrive(); cluster_wait(); }
 }
 
 // ------------------------------------------------------------------------------------------------ the same for few rows
@@ -1468,27 +1509,38 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
     return launch_after(few_kernel, dim3((unsigned)(p.nft * p.csize), (unsigned)tt), (unsigned)kWideThreads,
                         1024 + (size_t)p.ns * p.slot_bytes + rest, p.csize, c.st, tmW, tmIn, p);
   }
-  // rows of a tile: cycles of the busiest SM, a slab's operands arriving at 64 bytes a cycle or its MMAs, whichever is longer
+  // CTAs by themselves or in pairs, and the rows of a tile: cycles of the busiest SM, a slab's operands arriving at 64 bytes a cycle or its
+  // MMAs, whichever is longer
   double best = 1e30;
-  for (int bn = 32; bn <= 256; bn *= 2) {
-    const int64_t tiles = (int64_t)p.nft * ((c.N + bn - 1) / bn);
-    const double slab = 2.0 * (128 + bn) > (bn <= 64 ? 300.0 : bn <= 128 ? 330.0 : 560.0) ? 2.0 * (128 + bn) : bn <= 64 ? 300.0 : bn <= 128 ? 330.0 : 560.0;
-    const double t = (double)((tiles + sms - 1) / sms) * (p.nk + 2) * slab + 3000.0;
-    if (t < best) { best = t; p.bn = bn; }
-  }
+  bool pair = false;
+  for (int two = 0; two < 2; ++two)
+    for (int bn = 32 << two; bn <= 256; bn *= 2) {
+      const int64_t tiles = (int64_t)((P + (128 << two) - 1) / (128 << two)) * ((c.N + bn - 1) / bn);
+      const double mma = bn <= 64 ? 300.0 : bn <= 128 ? 330.0 : 560.0, arrive = 2.0 * (128 + (bn >> two));
+      const double t = (double)((tiles + (sms >> two) - 1) / (sms >> two)) * (p.nk + 2) * (arrive > mma ? arrive : mma) + (two ? 4500.0 : 3000.0);
+      if (t < best) { best = t; p.bn = bn; pair = two != 0; }
+    }
+  const int ctas = pair ? 2 : 1;
+  p.nft = (P + 128 * ctas - 1) / (128 * ctas);
   const int64_t tiles = (int64_t)p.nft * ((c.N + p.bn - 1) / p.bn);
   if (tiles > 0x7fffffffll) return AB_ERR_UNSUPPORTED;
   p.ntiles = (int)tiles;
-  p.slot_bytes = kABytes + p.bn * 128;
+  p.slot_bytes = kABytes + p.bn / ctas * 128;
   p.ns = 196608 / p.slot_bytes < kMaxStages ? 196608 / p.slot_bytes : kMaxStages;
   p.tmem_cols = 2 * pow2_cols(p.bn);
-  AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn));
-  AB_TRY(make_tensor_map_2d(&tmT, Tp, false, (uint64_t)c.N, 3 * rp, 3 * rp, 64, p.bn));
+  AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn / ctas));
+  AB_TRY(make_tensor_map_2d(&tmT, Tp, false, (uint64_t)c.N, 3 * rp, 3 * rp, 64, p.bn / ctas));
   AB_TRY(stack_map(&tmG, c, G, mn ? c.r : P, mn ? P : c.r, strideG, mn ? 64 : 128));
   AB_TRY(make_tensor_map_sw64(&tmOut, Out, (uint64_t)c.N, P, 32, 32));
-  AB_CUDA_OK(allow_smem(wide_kernel));
   const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + 4 * 2 * 2048 + kTbuf + sizeof(WideBars);
-  return launch_after(wide_kernel, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideThreads, smem, 1, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
+  if (pair) {
+    AB_CUDA_OK(allow_smem(wide_kernel<true>));
+    const int pairs = p.ntiles < sms / 2 ? p.ntiles : sms / 2;
+    return launch_after(wide_kernel<true>, (unsigned)(2 * pairs), (unsigned)kWideThreads, smem, 2, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
+  }
+  AB_CUDA_OK(allow_smem(wide_kernel<false>));
+  return launch_after(wide_kernel<false>, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideThreads, smem, 1, c.st, tmW, tmIn, tmG, tmT,
+                      tmOut, p);
 }
 
 // Slices of an adapter's rows, so that there are CTAs for every SM where adapters and tiles are few

@@ -352,3 +352,50 @@ def test_refusals():
         ab.ab_adapter_backward(x, dY[:, :8].contiguous(), W, A, B, ids)
     with pytest.raises(ab.AbError):
         ab.ab_adapter_forward(x, W, A, B, ids, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+# Rows beyond the kernel for few: 32 to 256 rows a tile, CTAs by themselves and in pairs, one tile a CTA and several
+WIDE = [(1025, 136, 200, 16, 3), (1300, 264, 328, 64, 5), (3000, 1000, 200, 24, 9), (1100, 2000, 136, 72, 4), (2500, 136, 72, 8, 2),
+        (9000, 520, 392, 40, 6), (20000, 264, 328, 136, 3)]
+
+
+@pytest.mark.parametrize("kind", ["one", "runs", "mixed", "alternate"])
+@pytest.mark.parametrize("N,m,n,r,L", WIDE)
+def test_many_rows(N, m, n, r, L, kind):
+    check(Case(N, m, n, r, L, kind, BF16))
+
+
+@pytest.mark.parametrize("kind", ["runs", "mixed"])
+@pytest.mark.parametrize("N,m,n,r,L", [(1300, 264, 328, 64, 4), (9000, 520, 392, 40, 4)])
+def test_nothing_leaks_between_many_rows(N, m, n, r, L, kind):
+    c = Case(N, m, n, r, L, kind, BF16)
+    c.ids[c.ids == 2] = 1
+    c.ids[400:405], c.ids[700:901] = 2, 2
+    c.map = torch.tensor(c.ids, dtype=torch.int32)
+    x, dY, W, A, B, ids, s = c.cuda()
+    y, T = ab.ab_adapter_forward(x, W, A, B, ids, scale=s, save_T=True)
+    dX, dA, dB = ab.ab_adapter_backward(x, dY, W, A, B, ids, scale=s)
+    bad = torch.tensor(c.ids == 2)
+    x2, dY2, A2, B2 = (t.clone() for t in (x, dY, A, B))
+    x2[bad.cuda()], dY2[bad.cuda()] = float("nan"), float("inf")
+    A2[2], B2[2] = float("inf"), float("nan")
+    y2, T2 = ab.ab_adapter_forward(x2, W, A2, B2, ids, scale=s, save_T=True)
+    dX2, dA2, dB2 = ab.ab_adapter_backward(x2, dY2, W, A2, B2, ids, scale=s)
+    ok, others = ~bad, [0, 1, 3]
+    for got, ref in ((y2, y), (T2, T), (dX2, dX)):
+        assert torch.equal(got.cpu()[ok], ref.cpu()[ok])
+    for got, ref in ((dA2, dA), (dB2, dB)):
+        assert torch.equal(got[others], ref[others]) and not torch.isfinite(got[2]).any()
+
+
+def test_bad_entries_among_many_rows():
+    c = Case(3000, 1000, 200, 24, 3, "mixed", BF16)
+    x, dY, W, A, B, ids, s = c.cuda()
+    ws = ab.workspace(ab.ab_adapter_workspace_bytes(x, A, B), "cuda")
+    for at, value in ((0, 3), (2999, -2), (1777, 2 ** 31 - 1)):
+        wrong, right = ids.clone(), ids.clone()
+        wrong[at], right[at] = value, -1
+        y, _ = ab.ab_adapter_forward(x, W, A, B, wrong, scale=s, ws=ws)
+        assert ab.workspace_status(ws) == ab.AB_ERR_INVALID_ARG
+        y2, _ = ab.ab_adapter_forward(x, W, A, B, right, scale=s, ws=ws)
+        assert ab.workspace_status(ws) == ab.AB_OK and torch.equal(y, y2)
