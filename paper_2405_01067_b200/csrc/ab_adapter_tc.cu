@@ -592,18 +592,30 @@ __device__ __forceinline__ void load_g(const OutParams& p, const bf16* __restric
     u[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
-__device__ __forceinline__ float sum16(const uint4 (&u)[2], const float* t) {
+// Two multiply-adds in one instruction.
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); }
+struct Pairs { uint64_t g[8]; };           // 16 bf16 values as pairs of fp32
+__device__ __forceinline__ Pairs unpack(const uint4 (&u)[2]) {
   const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
-  float s0 = 0.f, s1 = 0.f;
+  Pairs p;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p.g[e] = pack2(w[e] << 16, w[e] & 0xffff0000u);
+  return p;
+}
+__device__ __forceinline__ float sum16(const Pairs& p, const float* t) {
+  uint64_t s0 = 0, s1 = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float4 x = *reinterpret_cast<const float4*>(t + 4 * e);
-    s0 = fmaf(__uint_as_float(w[2 * e] << 16), x.x, s0);
-    s1 = fmaf(__uint_as_float(w[2 * e] & 0xffff0000u), x.y, s1);
-    s0 = fmaf(__uint_as_float(w[2 * e + 1] << 16), x.z, s0);
-    s1 = fmaf(__uint_as_float(w[2 * e + 1] & 0xffff0000u), x.w, s1);
+    const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(t + 4 * e);
+    s0 = fma2(p.g[2 * e], x.x, s0);
+    s1 = fma2(p.g[2 * e + 1], x.y, s1);
   }
-  return s0 + s1;
+  return (__uint_as_float((uint32_t)s0) + __uint_as_float((uint32_t)(s0 >> 32))) + (__uint_as_float((uint32_t)s1) + __uint_as_float((uint32_t)(s1 >> 32)));
 }
 __device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int64_t end, int f, int lane, float* Ts, float (&v)[kG]) {
   const int ff = f < p.P ? f : p.P - 1;       // a lane past the last feature reads what its neighbour reads
@@ -643,28 +655,29 @@ __device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int6
           const int kx = k1 + 16 < kn ? k0 + k1 + 16 : k0;
           load_g(p, ga, ff, kx, na);
           load_g(p, gb, ff, kx, nb);
+          const Pairs pa = unpack(ua), pb = unpack(ub);
 #pragma unroll
           for (int e = 0; e < kG; ++e) {
-            const float x = sum16(ua, Ts + e * 64 + k1), y = sum16(ub, Ts + e * 64 + k1);
+            const float x = sum16(pa, Ts + e * 64 + k1), y = sum16(pb, Ts + e * 64 + k1);
             v[e] += ((first >> e) & 1u) ? x : ((second >> e) & 1u) ? y : 0.f;
           }
 #pragma unroll
           for (int i = 0; i < 2; ++i) { ua[i] = na[i]; ub[i] = nb[i]; }
         }
       }
-    } else {                                   // an adapter a row, eight rows at a time
+    } else {                                   // an adapter a row, four rows at a time
       for (int k1 = 0; k1 < kn; k1 += 16) {
 #pragma unroll
-        for (int h = 0; h < kG; h += 8) {
-          uint4 u[8][2];
+        for (int h = 0; h < kG; h += 4) {
+          uint4 u[4][2];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
+          for (int e = 0; e < 4; ++e) {
             const int a = __shfl_sync(0xffffffffu, id, h + e);
             load_g(p, p.G + (a >= 0 ? a : 0) * p.strideG, ff, k0 + k1, u[e]);
           }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = sum16(u[e], Ts + (h + e) * 64 + k1);
+          for (int e = 0; e < 4; ++e) {
+            const float x = sum16(unpack(u[e]), Ts + (h + e) * 64 + k1);
             v[h + e] += ((live >> (h + e)) & 1u) ? x : 0.f;
           }
         }
@@ -702,15 +715,19 @@ __device__ __forceinline__ bool for_runs(int gid, int ngroups, int rp, F&& body)
 // kPair: two CTAs have a tile of 256 features x bn rows together, 128 features each, and load half of the rows each: 32 KB a slab and
 // CTA instead of 48, which arrive as fast as they are multiplied (512 cycles against 520; alone 768).  An MMA's columns then come in
 // 32s, and so do the groups.
+//
+// Eight epilogue warps, two for each quarter of the TMEM lanes, which take the tile's 32-row pieces in turn: mixed groups make some tiles'
+// epilogues longer than a tile's MMAs.
+constexpr int kWideAll = 320, kEpiWarps = 8;
 template <bool kPair>
-__global__ void __launch_bounds__(kWideThreads, 1)
+__global__ void __launch_bounds__(kWideAll, 1)
 wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmG,
             const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ OutParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint8_t* stg = ring + (size_t)p.ns * p.slot_bytes;              // per epilogue warp two tiles of 32 rows x 32 features
-  float* tbuf = reinterpret_cast<float*>(stg + 4 * 2 * 2048);     // and T of 16 rows
-  WideBars* b = reinterpret_cast<WideBars*>(tbuf + 4 * kG * 64);
+  uint8_t* stg = ring + (size_t)p.ns * p.slot_bytes;              // per epilogue warp a tile of 32 rows x 32 features
+  float* tbuf = reinterpret_cast<float*>(stg + kEpiWarps * 2048); // and T of 16 rows
+  WideBars* b = reinterpret_cast<WideBars*>(tbuf + kEpiWarps * kG * 64);
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   constexpr int kCtas = kPair ? 2 : 1, kGroup = kG * kCtas;       // rows of a group
   const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
@@ -719,7 +736,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   dep_launch();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.ns; ++i) { mbar_init(&b->full[i], 1); mbar_init(&b->empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&b->acc_full[i], 1); mbar_init(&b->acc_empty[i], 4 * kCtas); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&b->acc_full[i], 1); mbar_init(&b->acc_empty[i], kEpiWarps * kCtas); }
     b->abort_any = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tmW); tma_prefetch_desc(&tmIn); tma_prefetch_desc(&tmG); tma_prefetch_desc(&tmT); tma_prefetch_desc(&tmOut);
@@ -846,9 +863,9 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       }
     }
   } else {
-    const int qw = warp & 3;
+    const int qw = warp & 3, turn = (warp - 2) >> 2;
     const uint32_t lane_base = (uint32_t)(qw * 32) << 16;
-    uint8_t* my = stg + (size_t)(warp - 2) * 2 * 2048;
+    uint8_t* tile_s = stg + (size_t)(warp - 2) * 2048;
     const uint32_t acc_empty0 = kPair ? cluster_addr(smem_u32(&b->acc_empty[0]), 0) : 0u;
     auto give_back = [&](int buf) {
       tc_fence_before();
@@ -857,7 +874,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         if constexpr (kPair) mbar_arrive_cluster(acc_empty0 + (uint32_t)buf * 8); else mbar_arrive(&b->acc_empty[buf]);
       }
     };
-    int nst = 0, it = 0;
+    int it = 0;
     bool ok = true;
     dep_wait();                          // T is complete; and this kernel is done only after the ones before it
     for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step, ++it) {
@@ -874,14 +891,10 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1)) + lane_base;
       const bool live = f0 < p.P;
       const int n16 = p.bn / kG;
-      for (int g0 = 0; g0 < n16; g0 += 2) {
-        if (!live || (int64_t)row0 + g0 * kG >= p.N) {
-          if (g0 + 2 >= n16) give_back(buf);
-          continue;
-        }
-        uint8_t* tile_s = my + (nst & 1) * 2048;
-        ++nst;
-        if (lane == 0) tma_store_wait_read<1>();
+      bool given = false;
+      for (int g0 = 2 * turn; g0 < n16; g0 += 4) {
+        if (!live || (int64_t)row0 + g0 * kG >= p.N) break;
+        if (lane == 0) tma_store_wait_read<0>();
         __syncwarp();
         const bool simt = ((mixed >> g0) & 3u) != 0u;
         uint32_t v[2][16];
@@ -893,7 +906,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           tmem_ld16_nowait(tacc + g0 * kG + kG, v[1]);
         }
         tmem_wait_ld();
-        if (g0 + 2 >= n16) give_back(buf);         // the last columns are in registers
+        if (g0 + 4 >= n16 || (int64_t)row0 + (g0 + 4) * kG >= p.N) { give_back(buf); given = true; }      // the last columns are in registers
         if (!simt) {
           // eight rows (columns 8 j ..) of 32 features are four fragments; transposed they are 8 rows of 64 bytes, whose 16-byte pieces
           // lie where the swizzle puts them
@@ -931,6 +944,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           tma_store_commit();
         }
       }
+      if (!given) give_back(buf);
     }
     if (lane == 0) tma_store_wait_all();
     __syncwarp();
@@ -1402,8 +1416,6 @@ int pad16(int r) { return (r + 15) / 16 * 16; }
 int pow2_cols(int c) { int v = 32; while (v < c) v <<= 1; return v; }
 
 constexpr int kFewRows = 128;
-constexpr int kTbuf = 4 * kG * 64 * 4;
-
 // Whether few_kernel takes the rows: up to 128, and more while tiles of 64 rows leave an SM each for two CTAs of a cluster
 bool few_rows(int64_t N, int P) {
   if (N <= kFewRows) return true;
@@ -1526,20 +1538,21 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
   if (tiles > 0x7fffffffll) return AB_ERR_UNSUPPORTED;
   p.ntiles = (int)tiles;
   p.slot_bytes = kABytes + p.bn / ctas * 128;
-  p.ns = 196608 / p.slot_bytes < kMaxStages ? 196608 / p.slot_bytes : kMaxStages;
+  const int rest = 1024 + kEpiWarps * (2048 + kG * 64 * 4) + (int)sizeof(WideBars);
+  p.ns = (kMaxSmem - rest) / p.slot_bytes < kMaxStages ? (kMaxSmem - rest) / p.slot_bytes : kMaxStages;
   p.tmem_cols = 2 * pow2_cols(p.bn);
   AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn / ctas));
   AB_TRY(make_tensor_map_2d(&tmT, Tp, false, (uint64_t)c.N, 3 * rp, 3 * rp, 64, p.bn / ctas));
   AB_TRY(stack_map(&tmG, c, G, mn ? c.r : P, mn ? P : c.r, strideG, mn ? 64 : 128));
   AB_TRY(make_tensor_map_sw64(&tmOut, Out, (uint64_t)c.N, P, 32, 32));
-  const size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + 4 * 2 * 2048 + kTbuf + sizeof(WideBars);
+  const size_t smem = (size_t)p.ns * p.slot_bytes + rest;
   if (pair) {
     AB_CUDA_OK(allow_smem(wide_kernel<true>));
     const int pairs = p.ntiles < sms / 2 ? p.ntiles : sms / 2;
-    return launch_after(wide_kernel<true>, (unsigned)(2 * pairs), (unsigned)kWideThreads, smem, 2, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
+    return launch_after(wide_kernel<true>, (unsigned)(2 * pairs), (unsigned)kWideAll, smem, 2, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
   }
   AB_CUDA_OK(allow_smem(wide_kernel<false>));
-  return launch_after(wide_kernel<false>, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideThreads, smem, 1, c.st, tmW, tmIn, tmG, tmT,
+  return launch_after(wide_kernel<false>, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideAll, smem, 1, c.st, tmW, tmIn, tmG, tmT,
                       tmOut, p);
 }
 
