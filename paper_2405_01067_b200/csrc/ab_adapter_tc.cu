@@ -31,16 +31,18 @@ constexpr int kG = 16;                    // rows of a group
 __device__ __forceinline__ int clean_id(int a, int L) { return a >= 0 && a < L ? a : -1; }
 
 // What lane l < 16 returns for group l of the 256 rows from row0: its adapter, -1 (no adapter, or no rows), -2 (mixed).  Whole warp; lanes
-// 2 l and 2 l + 1 read the group's ids.  bad: an entry that is neither an adapter nor -1.
-__device__ __forceinline__ int group_ids(const int* __restrict__ ids, int64_t N, int L, int64_t row0, int lane, bool& bad) {
+// 2 l and 2 l + 1 read the group's ids (id: of rows 8 lane ..).  bad: an entry that is neither an adapter nor -1.
+__device__ __forceinline__ int group_ids(const int* __restrict__ ids, int64_t N, int L, int64_t row0, int lane, bool& bad, int (&id)[8]) {
   int first = -3, same = 1;
   bad = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int64_t row = row0 + 8 * lane + e;
+    id[e] = -1;
     if (row < N) {
       const int raw = ids[row], v = clean_id(raw, L);
       bad |= raw < -1 || raw >= L;
+      id[e] = v;
       if (first == -3) first = v;
       same &= v == first;
     }
@@ -367,7 +369,8 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
     const int whole = n <= kMaxAd;
     if (!whole) {                          // the uniform groups alone
       bool bad;
-      const int g = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+      int id[8];
+      const int g = group_ids(p.ids, p.N, p.L, row0, lane, bad, id);
       n = 0;
       const int ng = p.tile_rows / kG;
       for (int i = 0; i < ng; ++i) {
@@ -570,26 +573,29 @@ struct OutParams {
   int* status;
 };
 
-// v[e] += sum_k G_a(f, k) T[row][k] for 16 rows from row0 (those below `end`), each with its own adapter; lane = output feature f.  T by way
-// of a piece of shared memory of the warp (16 x 64 floats), 64 values at a time.  Every sum is formed for every row that shares a loop
-// and chosen afterwards, not multiplied by zero: straight code, whose many independent sums hide each other's latency.
-__device__ __forceinline__ void load_g(const OutParams& p, const bf16* __restrict__ g, int f, int k0, uint4 (&u)[2]) {
-  // 16 values from k0, or 8 where r ends there
+// acc[32 e + lane] += sum_k G_a(f, k) T[row0 + e][k] for 16 rows, each with its own adapter (id: lane l < 16 has row l's, -1 where there is
+// none or no row); lane = output feature f.  Adapter by adapter: 64 of its values are in registers while its rows are gone through, T by
+// way of a piece of shared memory of the warp (Ts, 16 x 64 floats), the next adapter's values on their way.  Loops, not straight code:
+// this runs once in a while, and unrolled over the rows a call took 18,500 cycles at rank 64, most of them for fetching instructions.
+template <int kN>                          // 8 kN values from k0, as many as there are
+__device__ __forceinline__ void load_g(const OutParams& p, const bf16* __restrict__ g, int f, int k0, uint4 (&u)[kN]) {
   if (!p.mn) {
     const uint4* q = reinterpret_cast<const uint4*>(g + (int64_t)f * p.r + k0);
-    u[0] = q[0];
-    u[1] = k0 + 8 < p.r ? q[1] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) u[i] = k0 + 8 * i < p.r ? q[i] : make_uint4(0u, 0u, 0u, 0u);
   } else {
     const unsigned short* q = reinterpret_cast<const unsigned short*>(g) + (int64_t)k0 * p.P + f;
-    uint32_t w[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool in = k0 + 2 * e < p.r;
-      const uint32_t lo = in ? q[(int64_t)(2 * e) * p.P] : 0u, hi = in ? q[(int64_t)(2 * e + 1) * p.P] : 0u;
-      w[e] = lo | (hi << 16);
+    for (int i = 0; i < kN; ++i) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = k0 + 8 * i < p.r;
+        const uint32_t lo = in ? q[(int64_t)(8 * i + 2 * e) * p.P] : 0u, hi = in ? q[(int64_t)(8 * i + 2 * e + 1) * p.P] : 0u;
+        w[e] = lo | (hi << 16);
+      }
+      u[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    u[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    u[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
 // Two multiply-adds in one instruction.
@@ -599,89 +605,68 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return d;
 }
 __device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); }
-struct Pairs { uint64_t g[8]; };           // 16 bf16 values as pairs of fp32
-__device__ __forceinline__ Pairs unpack(const uint4 (&u)[2]) {
-  const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
-  Pairs p;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) p.g[e] = pack2(w[e] << 16, w[e] & 0xffff0000u);
-  return p;
-}
-__device__ __forceinline__ float sum16(const Pairs& p, const float* t) {
-  uint64_t s0 = 0, s1 = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(t + 4 * e);
-    s0 = fma2(p.g[2 * e], x.x, s0);
-    s1 = fma2(p.g[2 * e + 1], x.y, s1);
-  }
-  return (__uint_as_float((uint32_t)s0) + __uint_as_float((uint32_t)(s0 >> 32))) + (__uint_as_float((uint32_t)s1) + __uint_as_float((uint32_t)(s1 >> 32)));
-}
-__device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int64_t end, int f, int lane, float* Ts, float (&v)[kG]) {
+__device__ __forceinline__ float both(uint64_t s) { return __uint_as_float((uint32_t)s) + __uint_as_float((uint32_t)(s >> 32)); }
+__device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int id, int f, int lane, float* Ts, float* acc) {
   const int ff = f < p.P ? f : p.P - 1;       // a lane past the last feature reads what its neighbour reads
-  const int rows = (int)(end - row0 < kG ? end - row0 : kG);
-  const int id = lane < rows ? clean_id(p.ids[row0 + lane], p.L) : -1;
   const unsigned live = __ballot_sync(0xffffffffu, id >= 0);
   if (live == 0u) return;
   const unsigned same = __match_any_sync(0xffffffffu, id);       // every lane, before any condition
   const unsigned heads = __ballot_sync(0xffffffffu, id >= 0 && lane == __ffs(same) - 1);   // an adapter's first row
-  const int adapters = __popc(heads);
+  const int trow = lane >> 1, tcol = (lane & 1) * 4;             // a row of T in two lanes' hands
+  const float* Trow = p.T + (row0 + trow) * p.r + tcol;
+  const bool tlive = (live >> trow) & 1u;
+#pragma unroll 1
   for (int k0 = 0; k0 < p.r; k0 += 64) {
     const int kn = p.r - k0 < 64 ? p.r - k0 : 64;
+    // T, and the values of the first two adapters: one trip to memory, which takes 2000 to 3000 cycles beside the tiles' loads
+    unsigned left = heads;
+    int h = __ffs(left) - 1;
+    left &= left - 1;
+    int h1 = __ffs(left) - 1;
+    uint4 cur[8], next[8];
+    float4 tv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) tv[i] = tlive && 8 * i < kn ? *reinterpret_cast<const float4*>(Trow + k0 + 8 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+    load_g(p, p.G + __shfl_sync(0xffffffffu, id, h) * p.strideG, ff, k0, cur);
+    if (h1 >= 0) load_g(p, p.G + __shfl_sync(0xffffffffu, id, h1) * p.strideG, ff, k0, next);
     __syncwarp();
-    // a row in two lanes' hands; what r does not fill of the last 16 values is 0
-    {
-      const int e = lane >> 1;
-      for (int c = (lane & 1) * 4; c < ((kn + 15) & ~15); c += 8)
-        *reinterpret_cast<float4*>(Ts + e * 64 + c) =
-            e < rows && c < kn ? *reinterpret_cast<const float4*>(p.T + (row0 + e) * p.r + k0 + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<float4*>(Ts + trow * 64 + tcol + 8 * i) = tv[i];
     __syncwarp();
-    if (adapters <= 4) {                       // the values of two adapters at a time, for all rows
-      unsigned left = heads;
-      while (left) {
-        const int h0 = __ffs(left) - 1;
-        left &= left - 1;
-        const int h1 = left ? __ffs(left) - 1 : h0;
-        if (left) left &= left - 1;
-        const int a0 = __shfl_sync(0xffffffffu, id, h0), a1 = __shfl_sync(0xffffffffu, id, h1);
-        const unsigned first = __ballot_sync(0xffffffffu, id == a0), second = __ballot_sync(0xffffffffu, id == a1);
-        const bf16 *ga = p.G + a0 * p.strideG, *gb = p.G + a1 * p.strideG;
-        uint4 ua[2], ub[2];
-        load_g(p, ga, ff, k0, ua);
-        load_g(p, gb, ff, k0, ub);
-        for (int k1 = 0; k1 < kn; k1 += 16) {
-          uint4 na[2], nb[2];
-          const int kx = k1 + 16 < kn ? k0 + k1 + 16 : k0;
-          load_g(p, ga, ff, kx, na);
-          load_g(p, gb, ff, kx, nb);
-          const Pairs pa = unpack(ua), pb = unpack(ub);
+#pragma unroll 1
+    while (true) {
+      uint64_t g[32];
 #pragma unroll
-          for (int e = 0; e < kG; ++e) {
-            const float x = sum16(pa, Ts + e * 64 + k1), y = sum16(pb, Ts + e * 64 + k1);
-            v[e] += ((first >> e) & 1u) ? x : ((second >> e) & 1u) ? y : 0.f;
-          }
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t w[4] = {cur[i].x, cur[i].y, cur[i].z, cur[i].w};
 #pragma unroll
-          for (int i = 0; i < 2; ++i) { ua[i] = na[i]; ub[i] = nb[i]; }
-        }
+        for (int e = 0; e < 4; ++e) g[4 * i + e] = pack2(w[e] << 16, w[e] & 0xffff0000u);
       }
-    } else {                                   // an adapter a row, four rows at a time
-      for (int k1 = 0; k1 < kn; k1 += 16) {
+      unsigned rows = __shfl_sync(0xffffffffu, same, h);          // the rows with this adapter
+#pragma unroll 1
+      while (rows) {
+        const int e = __ffs(rows) - 1;
+        rows &= rows - 1;
+        const ulonglong2* t = reinterpret_cast<const ulonglong2*>(Ts + e * 64);
+        uint64_t s0 = 0, s1 = 0, s2 = 0, s3 = 0;
 #pragma unroll
-        for (int h = 0; h < kG; h += 4) {
-          uint4 u[4][2];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int a = __shfl_sync(0xffffffffu, id, h + e);
-            load_g(p, p.G + (a >= 0 ? a : 0) * p.strideG, ff, k0 + k1, u[e]);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = sum16(unpack(u[e]), Ts + (h + e) * 64 + k1);
-            v[h + e] += ((live >> (h + e)) & 1u) ? x : 0.f;
-          }
+        for (int i = 0; i < 8; ++i) {
+          if (8 * i >= kn) break;
+          const ulonglong2 x = t[2 * i], y = t[2 * i + 1];
+          s0 = fma2(g[4 * i], x.x, s0);
+          s1 = fma2(g[4 * i + 1], x.y, s1);
+          s2 = fma2(g[4 * i + 2], y.x, s2);
+          s3 = fma2(g[4 * i + 3], y.y, s3);
         }
+        acc[32 * e + lane] += (both(s0) + both(s1)) + (both(s2) + both(s3));
       }
+      if (h1 < 0) break;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) cur[i] = next[i];
+      h = h1;
+      left &= left - 1;
+      h1 = __ffs(left) - 1;
+      if (h1 >= 0) load_g(p, p.G + __shfl_sync(0xffffffffu, id, h1) * p.strideG, ff, k0, next);
     }
   }
 }
@@ -716,18 +701,18 @@ __device__ __forceinline__ bool for_runs(int gid, int ngroups, int rp, F&& body)
 // CTA instead of 48, which arrive as fast as they are multiplied (512 cycles against 520; alone 768).  An MMA's columns then come in
 // 32s, and so do the groups.
 //
-// Eight epilogue warps, two for each quarter of the TMEM lanes, which take the tile's 32-row pieces in turn: mixed groups make some tiles'
-// epilogues longer than a tile's MMAs.
-constexpr int kWideAll = 320, kEpiWarps = 8;
+// The ring is as deep as shared memory lets it be: beside the other SMs' loads a load takes 2000 to 3000 cycles (8191 x 4096 x 4096, four
+// slabs of 32 KB 194 us, five 169).
+constexpr int kEpiWarps = 4;
+constexpr int kEpiBytes = 2048 + (kG * 64 + kG * 32) * 4;        // of an epilogue warp: a tile of 32 rows x 32 features, T and sums of 16 rows
 template <bool kPair>
-__global__ void __launch_bounds__(kWideAll, 1)
+__global__ void __launch_bounds__(kWideThreads, 1)
 wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmG,
             const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ OutParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint8_t* stg = ring + (size_t)p.ns * p.slot_bytes;              // per epilogue warp a tile of 32 rows x 32 features
-  float* tbuf = reinterpret_cast<float*>(stg + kEpiWarps * 2048); // and T of 16 rows
-  WideBars* b = reinterpret_cast<WideBars*>(tbuf + kEpiWarps * kG * 64);
+  uint8_t* stg = ring + (size_t)p.ns * p.slot_bytes;
+  WideBars* b = reinterpret_cast<WideBars*>(stg + kEpiWarps * kEpiBytes);
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   constexpr int kCtas = kPair ? 2 : 1, kGroup = kG * kCtas;       // rows of a group
   const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
@@ -751,8 +736,8 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   const uint32_t tmem = uniform(*reinterpret_cast<volatile uint32_t*>(&b->tmem_base));
   const int ngroups = p.bn / kGroup;
   // lane g: the adapter of group g, -1 none, -2 mixed
-  auto groups = [&](int row0, bool& bad) {
-    int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad);
+  auto groups = [&](int row0, bool& bad, int (&id)[8]) {
+    int gid = group_ids(p.ids, p.N, p.L, row0, lane, bad, id);
     if constexpr (kPair) {
       const int x = __shfl_sync(0xffffffffu, gid, (2 * lane) & 31), y = __shfl_sync(0xffffffffu, gid, (2 * lane + 1) & 31);
       // a second half behind the last row goes with the first
@@ -777,7 +762,8 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step) {
       const int f0 = ((tile % p.nft) * kCtas + rank) * 128, row0 = (tile / p.nft) * p.bn;
       bool bad;
-      const int gid = groups(row0, bad);
+      int id[8];
+      const int gid = groups(row0, bad, id);
       for (int i = 0; i < p.nk; ++i) {
         if (!mbar_wait_warp(&b->empty[slot], ph)) { raise(&b->abort_any, p.status); ok = false; break; }
         if (elect_one()) {
@@ -823,7 +809,8 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step, ++it) {
         const int row0 = (tile / p.nft) * p.bn, buf = it & 1;
         bool bad;
-        const int gid = groups(row0, bad);
+        int id[8];
+        const int gid = groups(row0, bad, id);
         if (!mbar_wait_warp(&b->acc_empty[buf], ((it >> 1) & 1) ^ 1)) { raise(&b->abort_any, p.status); break; }
         tc_fence_after();
         const uint32_t tacc = tmem + (uint32_t)(buf * (p.tmem_cols >> 1));
@@ -863,9 +850,11 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       }
     }
   } else {
-    const int qw = warp & 3, turn = (warp - 2) >> 2;
+    const int qw = warp & 3;
     const uint32_t lane_base = (uint32_t)(qw * 32) << 16;
-    uint8_t* tile_s = stg + (size_t)(warp - 2) * 2048;
+    uint8_t* tile_s = stg + (size_t)(warp - 2) * kEpiBytes;
+    float* Ts = reinterpret_cast<float*>(tile_s + 2048);
+    float* sums = Ts + kG * 64;
     const uint32_t acc_empty0 = kPair ? cluster_addr(smem_u32(&b->acc_empty[0]), 0) : 0u;
     auto give_back = [&](int buf) {
       tc_fence_before();
@@ -880,7 +869,8 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
     for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step, ++it) {
       const int ftile = (tile % p.nft) * kCtas + rank, f0 = ftile * 128 + qw * 32, row0 = (tile / p.nft) * p.bn, buf = it & 1;
       bool bad;
-      const int gid = groups(row0, bad);
+      int id[8];
+      const int gid = groups(row0, bad, id);
       const bool any_bad = __any_sync(0xffffffffu, bad && lane * 8 < p.bn);
       if (ftile == 0 && qw == 0 && any_bad && lane == 0) atomicExch(p.status, (int)AB_ERR_INVALID_ARG);
       // bit g: the adapters' part of the 16 rows from 16 g goes over the fp32 pipes
@@ -892,22 +882,17 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       const bool live = f0 < p.P;
       const int n16 = p.bn / kG;
       bool given = false;
-      for (int g0 = 2 * turn; g0 < n16; g0 += 4) {
+      for (int g0 = 0; g0 < n16; g0 += 2) {
         if (!live || (int64_t)row0 + g0 * kG >= p.N) break;
         if (lane == 0) tma_store_wait_read<0>();
         __syncwarp();
-        const bool simt = ((mixed >> g0) & 3u) != 0u;
-        uint32_t v[2][16];
-        if (!simt) {                     // features 0..15 and 16..31 of the warp, 32 rows
+        const bool last = g0 + 2 >= n16 || (int64_t)row0 + (g0 + 2) * kG >= p.N;      // the accumulator's last columns
+        if (((mixed >> g0) & 3u) == 0u) {
+          uint32_t v[2][16];             // features 0..15 and 16..31 of the warp, 32 rows
           tmem_ld_16x32_nowait(tacc + g0 * kG, v[0]);
           tmem_ld_16x32_nowait(tacc + (16u << 16) + g0 * kG, v[1]);
-        } else {                         // a feature a lane, 16 + 16 rows
-          tmem_ld16_nowait(tacc + g0 * kG, v[0]);
-          tmem_ld16_nowait(tacc + g0 * kG + kG, v[1]);
-        }
-        tmem_wait_ld();
-        if (g0 + 4 >= n16 || (int64_t)row0 + (g0 + 4) * kG >= p.N) { give_back(buf); given = true; }      // the last columns are in registers
-        if (!simt) {
+          tmem_wait_ld();
+          if (last) { give_back(buf); given = true; }
           // eight rows (columns 8 j ..) of 32 features are four fragments; transposed they are 8 rows of 64 bytes, whose 16-byte pieces
           // lie where the swizzle puts them
 #pragma unroll
@@ -923,17 +908,26 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
             stmatrix_x4_trans(smem_u32(tile_s) + r * 64 + piece * 16, w[0], w[1], w[2], w[3]);
           }
         } else {
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {  // a feature a lane, 16 rows
+            float v[kG];
+            tmem_ld16(tacc + (g0 + h) * kG, v);
+            if (last && h == 1) { give_back(buf); given = true; }
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float d[kG];
+            for (int e = 0; e < kG; ++e) sums[e * 32 + lane] = v[e];
+            if (((mixed >> (g0 + h)) & 1u) && (int64_t)row0 + (g0 + h) * kG < p.N) {
+              int mine = -1;             // lane l < 16: the adapter of row l of the group, which lane 2 (g0 + h) + l / 8 has
 #pragma unroll
-            for (int e = 0; e < kG; ++e) d[e] = __uint_as_float(v[h][e]);
-            if (((mixed >> (g0 + h)) & 1u) && (int64_t)row0 + (g0 + h) * kG < p.N)
-              add_mixed(p, (int64_t)row0 + (g0 + h) * kG, p.N, f0 + lane, lane, tbuf + (warp - 2) * kG * 64, d);
-#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int x = __shfl_sync(0xffffffffu, id[e], 2 * (g0 + h) + ((lane & 15) >> 3));
+                if (lane < kG && (lane & 7) == e) mine = x;
+              }
+              add_mixed(p, (int64_t)row0 + (g0 + h) * kG, mine, f0 + lane, lane, Ts, sums);
+            }
+#pragma unroll 4
             for (int e = 0; e < kG; ++e) {
               const int r = h * kG + e;
-              *reinterpret_cast<bf16*>(tile_s + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2) = __float2bfloat16_rn(d[e]);
+              *reinterpret_cast<bf16*>(tile_s + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2) = __float2bfloat16_rn(sums[e * 32 + lane]);
             }
           }
         }
@@ -1538,7 +1532,7 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
   if (tiles > 0x7fffffffll) return AB_ERR_UNSUPPORTED;
   p.ntiles = (int)tiles;
   p.slot_bytes = kABytes + p.bn / ctas * 128;
-  const int rest = 1024 + kEpiWarps * (2048 + kG * 64 * 4) + (int)sizeof(WideBars);
+  const int rest = 1024 + kEpiWarps * kEpiBytes + (int)sizeof(WideBars);
   p.ns = (kMaxSmem - rest) / p.slot_bytes < kMaxStages ? (kMaxSmem - rest) / p.slot_bytes : kMaxStages;
   p.tmem_cols = 2 * pow2_cols(p.bn);
   AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.bn / ctas));
@@ -1549,10 +1543,10 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
   if (pair) {
     AB_CUDA_OK(allow_smem(wide_kernel<true>));
     const int pairs = p.ntiles < sms / 2 ? p.ntiles : sms / 2;
-    return launch_after(wide_kernel<true>, (unsigned)(2 * pairs), (unsigned)kWideAll, smem, 2, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
+    return launch_after(wide_kernel<true>, (unsigned)(2 * pairs), (unsigned)kWideThreads, smem, 2, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
   }
   AB_CUDA_OK(allow_smem(wide_kernel<false>));
-  return launch_after(wide_kernel<false>, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideAll, smem, 1, c.st, tmW, tmIn, tmG, tmT,
+  return launch_after(wide_kernel<false>, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideThreads, smem, 1, c.st, tmW, tmIn, tmG, tmT,
                       tmOut, p);
 }
 
