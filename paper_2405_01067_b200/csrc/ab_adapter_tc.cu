@@ -189,7 +189,7 @@ struct ProjParams {
   const float* scale; const int* ids;
   float* T; bf16* P;                        // T: N x r; P: N x 3 rp
   int r, rp, L;
-  int want_T;                               // T (fp32) is wanted in every row, else in those of mixed groups
+  int want_T;                               // T is wanted in fp32 too
   int all_rows;                             // every row goes by rows_kernel
   int tile_rows;
   int unit;                                 // rows of a CTA of rows_kernel, a divisor of tile_rows
@@ -455,8 +455,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
       const int g0 = (int)__shfl_sync(0xffffffffu, a, lane & 16);
       const unsigned same = __ballot_sync(0xffffffffu, a == g0 || !live);
       const bool mixed = ((same >> (lane & 16)) & 0xffffu) != 0xffffu;
-      const bool mixed32 = same != 0xffffffffu || (int)__shfl_sync(0xffffffffu, a, 0) != (int)__shfl_sync(0xffffffffu, a, 16);
-      b->row_ad[lrow] = !live || (mixed && !b->whole) ? -2 : p.want_T || mixed32 ? (a < 0 ? 0x7fffffff : a | 0x40000000) : a;
+      b->row_ad[lrow] = !live || (mixed && !b->whole) ? -2 : p.want_T ? (a < 0 ? 0x7fffffff : a | 0x40000000) : a;
     }
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
@@ -565,7 +564,7 @@ struct OutParams {
   int64_t N; int P, K, nk;                  // rows, output features, reduction of the shared product, its slabs
   int r, rp, L;
   int mn;                                   // 0: W is P x K and G_a P x r; 1: W is K x P and G_a r x P
-  const int* ids; const float* T;
+  const int* ids; const float* T; const bf16* Tp;      // T in fp32 (few_kernel), in pieces (wide_kernel)
   const bf16* G; int64_t strideG;
   bf16* Out;
   int bn, nft, ntiles, ns, slot_bytes, tmem_cols;
@@ -573,100 +572,106 @@ struct OutParams {
   int* status;
 };
 
-// acc[32 e + lane] += sum_k G_a(f, k) T[row0 + e][k] for 16 rows, each with its own adapter (id: lane l < 16 has row l's, -1 where there is
-// none or no row); lane = output feature f.  Adapter by adapter: 64 of its values are in registers while its rows are gone through, T by
-// way of a piece of shared memory of the warp (Ts, 16 x 64 floats), the next adapter's values on their way.  Loops, not straight code:
-// this runs once in a while, and unrolled over the rows a call took 18,500 cycles at rank 64, most of them for fetching instructions.
-template <int kN>                          // 8 kN values from k0, as many as there are
-__device__ __forceinline__ void load_g(const OutParams& p, const bf16* __restrict__ g, int f, int k0, uint4 (&u)[kN]) {
-  if (!p.mn) {
-    const uint4* q = reinterpret_cast<const uint4*>(g + (int64_t)f * p.r + k0);
+// A warp's 32 features of 32 rows with mixed adapters, as it holds them between TMEM and the result (v[h][4 j + i]: feature 16 h + lane / 4 (+ 8
+// for i >= 2), row 8 j + 2 (lane % 4) (+ 1 for odd i), which is how mma.sync lays out a 16 x 8 accumulator): v += G_a T^T for the rows
+// of each adapter that occurs.  id: lane l has row l's adapter, -1 where there is nothing to add.  The product is formed for all rows
+// of eight that have one of the adapter's, and each row takes its own: nothing is masked by zeros.
+//
+// Operands come from global memory straight into fragments, for 64 values of r at once.  Beside the tiles' loads a trip to memory takes 2000
+// to 3000 cycles, and shared memory is busy with them and the MMAs' operands: sums over the fp32 pipes with T in shared memory
+// took 13,000 cycles for 16 rows at rank 64.
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ void load_g(const OutParams& p, int a, int f0, int k0, int kn, int lane, uint32_t (&u)[2][4][4]) {
+  const bf16* g = p.G + a * p.strideG;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) u[i] = k0 + 8 * i < p.r ? q[i] : make_uint4(0u, 0u, 0u, 0u);
-  } else {
-    const unsigned short* q = reinterpret_cast<const unsigned short*>(g) + (int64_t)k0 * p.P + f;
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      uint32_t w[4];
+    for (int x = 0; x < 2; ++x) {            // a feature past the last one reads what the last one does
+      const int f = f0 + 16 * h + 8 * x + (lane >> 2), ff = f < p.P ? f : p.P - 1;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool in = k0 + 8 * i < p.r;
-        const uint32_t lo = in ? q[(int64_t)(8 * i + 2 * e) * p.P] : 0u, hi = in ? q[(int64_t)(8 * i + 2 * e + 1) * p.P] : 0u;
-        w[e] = lo | (hi << 16);
-      }
-      u[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int k = k0 + 16 * kk + 8 * y + 2 * (lane & 3);
+          uint32_t w = 0u;
+          if (16 * kk + 8 * y < kn) {
+            if (!p.mn) {
+              w = *reinterpret_cast<const uint32_t*>(g + (int64_t)ff * p.r + k);
+            } else {
+              const unsigned short* q = reinterpret_cast<const unsigned short*>(g) + (int64_t)k * p.P + ff;
+              w = (uint32_t)q[0] | ((uint32_t)q[p.P] << 16);
+            }
+          }
+          u[h][kk][2 * y + x] = w;
+        }
     }
-  }
 }
-// Two multiply-adds in one instruction.
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); }
-__device__ __forceinline__ float both(uint64_t s) { return __uint_as_float((uint32_t)s) + __uint_as_float((uint32_t)(s >> 32)); }
-__device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int id, int f, int lane, float* Ts, float* acc) {
-  const int ff = f < p.P ? f : p.P - 1;       // a lane past the last feature reads what its neighbour reads
+__device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int id, int f0, int lane, uint32_t (&v)[2][16]) {
   const unsigned live = __ballot_sync(0xffffffffu, id >= 0);
   if (live == 0u) return;
   const unsigned same = __match_any_sync(0xffffffffu, id);       // every lane, before any condition
   const unsigned heads = __ballot_sync(0xffffffffu, id >= 0 && lane == __ffs(same) - 1);   // an adapter's first row
-  const int trow = lane >> 1, tcol = (lane & 1) * 4;             // a row of T in two lanes' hands
-  const float* Trow = p.T + (row0 + trow) * p.r + tcol;
-  const bool tlive = (live >> trow) & 1u;
 #pragma unroll 1
   for (int k0 = 0; k0 < p.r; k0 += 64) {
-    const int kn = p.r - k0 < 64 ? p.r - k0 : 64;
-    // T, and the values of the first two adapters: one trip to memory, which takes 2000 to 3000 cycles beside the tiles' loads
+    const int kn = p.r - k0 < 64 ? p.r - k0 : 64;                // a multiple of 8; T's pieces have zeros up to the next 16
     unsigned left = heads;
     int h = __ffs(left) - 1;
     left &= left - 1;
-    int h1 = __ffs(left) - 1;
-    uint4 cur[8], next[8];
-    float4 tv[8];
+    uint32_t t[2][4][4][2], g[2][4][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) tv[i] = tlive && 8 * i < kn ? *reinterpret_cast<const float4*>(Trow + k0 + 8 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
-    load_g(p, p.G + __shfl_sync(0xffffffffu, id, h) * p.strideG, ff, k0, cur);
-    if (h1 >= 0) load_g(p, p.G + __shfl_sync(0xffffffffu, id, h1) * p.strideG, ff, k0, next);
-    __syncwarp();
+    for (int j = 0; j < 4; ++j) {
+      int64_t row = row0 + 8 * j + (lane >> 2);
+      if (row >= p.N) row = p.N - 1;
+      const bf16* q = p.Tp + row * 3 * p.rp + k0 + 2 * (lane & 3);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) *reinterpret_cast<float4*>(Ts + trow * 64 + tcol + 8 * i) = tv[i];
-    __syncwarp();
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            t[c][j][kk][y] = 16 * kk < kn ? *reinterpret_cast<const uint32_t*>(q + c * p.rp + 16 * kk + 8 * y) : 0u;
+    }
+    load_g(p, __shfl_sync(0xffffffffu, id, h), f0, k0, kn, lane, g);
 #pragma unroll 1
     while (true) {
-      uint64_t g[32];
+      const unsigned rows = __shfl_sync(0xffffffffu, same, h) & live;
+      float c[2][4][4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t w[4] = {cur[i].x, cur[i].y, cur[i].z, cur[i].w};
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) g[4 * i + e] = pack2(w[e] << 16, w[e] & 0xffff0000u);
-      }
-      unsigned rows = __shfl_sync(0xffffffffu, same, h);          // the rows with this adapter
-#pragma unroll 1
-      while (rows) {
-        const int e = __ffs(rows) - 1;
-        rows &= rows - 1;
-        const ulonglong2* t = reinterpret_cast<const ulonglong2*>(Ts + e * 64);
-        uint64_t s0 = 0, s1 = 0, s2 = 0, s3 = 0;
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (8 * i >= kn) break;
-          const ulonglong2 x = t[2 * i], y = t[2 * i + 1];
-          s0 = fma2(g[4 * i], x.x, s0);
-          s1 = fma2(g[4 * i + 1], x.y, s1);
-          s2 = fma2(g[4 * i + 2], y.x, s2);
-          s3 = fma2(g[4 * i + 3], y.y, s3);
+          for (int i = 0; i < 4; ++i) c[m][j][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (((rows >> (8 * j)) & 0xffu) == 0u) continue;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          if (16 * kk >= kn) break;
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            mma_16x8x16(c[m][j], g[m][kk], t[1][j][kk]);
+            mma_16x8x16(c[m][j], g[m][kk], t[0][j][kk]);
+          }
         }
-        acc[32 * e + lane] += (both(s0) + both(s1)) + (both(s2) + both(s3));
       }
-      if (h1 < 0) break;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) cur[i] = next[i];
-      h = h1;
+      h = __ffs(left) - 1;
       left &= left - 1;
-      h1 = __ffs(left) - 1;
-      if (h1 >= 0) load_g(p, p.G + __shfl_sync(0xffffffffu, id, h1) * p.strideG, ff, k0, next);
+      if (h >= 0) load_g(p, __shfl_sync(0xffffffffu, id, h), f0, k0, kn, lane, g);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool take = (rows >> (8 * j + 2 * (lane & 3) + (i & 1))) & 1u;
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+            if (take) v[m][4 * j + i] = __float_as_uint(__uint_as_float(v[m][4 * j + i]) + c[m][j][i]);
+        }
+      if (h < 0) break;
     }
   }
 }
@@ -704,7 +709,7 @@ __device__ __forceinline__ bool for_runs(int gid, int ngroups, int rp, F&& body)
 // The ring is as deep as shared memory lets it be: beside the other SMs' loads a load takes 2000 to 3000 cycles (8191 x 4096 x 4096, four
 // slabs of 32 KB 194 us, five 169).
 constexpr int kEpiWarps = 4;
-constexpr int kEpiBytes = 2048 + (kG * 64 + kG * 32) * 4;        // of an epilogue warp: a tile of 32 rows x 32 features, T and sums of 16 rows
+constexpr int kEpiBytes = 2 * 2048;        // of an epilogue warp: two tiles of 32 rows x 32 features
 template <bool kPair>
 __global__ void __launch_bounds__(kWideThreads, 1)
 wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmG,
@@ -852,9 +857,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   } else {
     const int qw = warp & 3;
     const uint32_t lane_base = (uint32_t)(qw * 32) << 16;
-    uint8_t* tile_s = stg + (size_t)(warp - 2) * kEpiBytes;
-    float* Ts = reinterpret_cast<float*>(tile_s + 2048);
-    float* sums = Ts + kG * 64;
+    uint8_t* my = stg + (size_t)(warp - 2) * kEpiBytes;
     const uint32_t acc_empty0 = kPair ? cluster_addr(smem_u32(&b->acc_empty[0]), 0) : 0u;
     auto give_back = [&](int buf) {
       tc_fence_before();
@@ -863,7 +866,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         if constexpr (kPair) mbar_arrive_cluster(acc_empty0 + (uint32_t)buf * 8); else mbar_arrive(&b->acc_empty[buf]);
       }
     };
-    int it = 0;
+    int nst = 0, it = 0;
     bool ok = true;
     dep_wait();                          // T is complete; and this kernel is done only after the ones before it
     for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step, ++it) {
@@ -884,52 +887,39 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       bool given = false;
       for (int g0 = 0; g0 < n16; g0 += 2) {
         if (!live || (int64_t)row0 + g0 * kG >= p.N) break;
-        if (lane == 0) tma_store_wait_read<0>();
+        uint8_t* tile_s = my + (nst & 1) * 2048;
+        ++nst;
+        if (lane == 0) tma_store_wait_read<1>();
         __syncwarp();
         const bool last = g0 + 2 >= n16 || (int64_t)row0 + (g0 + 2) * kG >= p.N;      // the accumulator's last columns
-        if (((mixed >> g0) & 3u) == 0u) {
-          uint32_t v[2][16];             // features 0..15 and 16..31 of the warp, 32 rows
-          tmem_ld_16x32_nowait(tacc + g0 * kG, v[0]);
-          tmem_ld_16x32_nowait(tacc + (16u << 16) + g0 * kG, v[1]);
-          tmem_wait_ld();
-          if (last) { give_back(buf); given = true; }
-          // eight rows (columns 8 j ..) of 32 features are four fragments; transposed they are 8 rows of 64 bytes, whose 16-byte pieces
-          // lie where the swizzle puts them
+        uint32_t v[2][16];               // features 0..15 and 16..31 of the warp, 32 rows
+        tmem_ld_16x32_nowait(tacc + g0 * kG, v[0]);
+        tmem_ld_16x32_nowait(tacc + (16u << 16) + g0 * kG, v[1]);
+        tmem_wait_ld();
+        if (last) { give_back(buf); given = true; }
+        const unsigned halves = (mixed >> g0) & 3u;
+        if (halves) {
+          int mine = -1;                 // row l of the 32, which lane 2 g0 + l / 8 has
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t w[4];
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              const __nv_bfloat162 x = __floats2bfloat162_rn(__uint_as_float(v[h >> 1][4 * j + 2 * (h & 1)]),
-                                                             __uint_as_float(v[h >> 1][4 * j + 2 * (h & 1) + 1]));
-              w[h] = *reinterpret_cast<const uint32_t*>(&x);
-            }
-            const int r = 8 * j + (lane & 7), piece = (lane >> 3) ^ ((r >> 1) & 3);
-            stmatrix_x4_trans(smem_u32(tile_s) + r * 64 + piece * 16, w[0], w[1], w[2], w[3]);
+          for (int e = 0; e < 8; ++e) {
+            const int x = __shfl_sync(0xffffffffu, id[e], 2 * g0 + (lane >> 3));
+            if ((lane & 7) == e && ((halves >> (lane >> 4)) & 1u)) mine = x;
           }
-        } else {
-#pragma unroll 1
-          for (int h = 0; h < 2; ++h) {  // a feature a lane, 16 rows
-            float v[kG];
-            tmem_ld16(tacc + (g0 + h) * kG, v);
-            if (last && h == 1) { give_back(buf); given = true; }
+          add_mixed(p, (int64_t)row0 + g0 * kG, mine, f0, lane, v);
+        }
+        // eight rows (columns 8 j ..) of 32 features are four fragments; transposed they are 8 rows of 64 bytes, whose 16-byte pieces
+        // lie where the swizzle puts them
 #pragma unroll
-            for (int e = 0; e < kG; ++e) sums[e * 32 + lane] = v[e];
-            if (((mixed >> (g0 + h)) & 1u) && (int64_t)row0 + (g0 + h) * kG < p.N) {
-              int mine = -1;             // lane l < 16: the adapter of row l of the group, which lane 2 (g0 + h) + l / 8 has
+        for (int j = 0; j < 4; ++j) {
+          uint32_t w[4];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int x = __shfl_sync(0xffffffffu, id[e], 2 * (g0 + h) + ((lane & 15) >> 3));
-                if (lane < kG && (lane & 7) == e) mine = x;
-              }
-              add_mixed(p, (int64_t)row0 + (g0 + h) * kG, mine, f0 + lane, lane, Ts, sums);
-            }
-#pragma unroll 4
-            for (int e = 0; e < kG; ++e) {
-              const int r = h * kG + e;
-              *reinterpret_cast<bf16*>(tile_s + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2) = __float2bfloat16_rn(sums[e * 32 + lane]);
-            }
+          for (int h = 0; h < 4; ++h) {
+            const __nv_bfloat162 x = __floats2bfloat162_rn(__uint_as_float(v[h >> 1][4 * j + 2 * (h & 1)]),
+                                                           __uint_as_float(v[h >> 1][4 * j + 2 * (h & 1) + 1]));
+            w[h] = *reinterpret_cast<const uint32_t*>(&x);
           }
+          const int r = 8 * j + (lane & 7), piece = (lane >> 3) ^ ((r >> 1) & 3);
+          stmatrix_x4_trans(smem_u32(tile_s) + r * 64 + piece * 16, w[0], w[1], w[2], w[3]);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -1487,7 +1477,7 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
   OutParams p;
   std::memset(&p, 0, sizeof(p));
   const int rp = pad16(c.r);
-  p.N = c.N; p.P = P; p.K = K; p.nk = (K + 63) / 64; p.r = c.r; p.rp = rp; p.L = c.L; p.mn = mn ? 1 : 0; p.ids = c.ids; p.T = T;
+  p.N = c.N; p.P = P; p.K = K; p.nk = (K + 63) / 64; p.r = c.r; p.rp = rp; p.L = c.L; p.mn = mn ? 1 : 0; p.ids = c.ids; p.T = T; p.Tp = Tp;
   p.G = static_cast<const bf16*>(G); p.strideG = strideG; p.Out = static_cast<bf16*>(Out); p.status = status;
   p.nft = (P + 127) / 128;
   CUtensorMap tmW, tmIn, tmG, tmT, tmOut;
