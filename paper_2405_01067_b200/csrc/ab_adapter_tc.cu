@@ -120,7 +120,6 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint4* __restrict__ l
       put_pieces(P + row * 3 * rp + k, rp, v);
     }
     fence_proxy_async_all();
-    if (!first) dep_wait();          // this kernel is done only after the one before it
     return;
   }
   const int a = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -153,7 +152,9 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint4* __restrict__ l
     __syncthreads();
   }
   if (threadIdx.x == 0) count[a] = at;
-  if (!first) dep_wait();
+  // The kernel is done only after the one before it.  One block waits: were it all of them, those that find no room beside that kernel
+  // would not begin before it ends.
+  if (!first && blockIdx.x == 0) dep_wait();
 }
 
 // ------------------------------------------------------------------------------------------------ T of rows in mixed groups
@@ -708,10 +709,12 @@ __device__ __forceinline__ bool for_runs(int gid, int ngroups, int rp, F&& body)
 //
 // The ring is as deep as shared memory lets it be: beside the other SMs' loads a load takes 2000 to 3000 cycles (8191 x 4096 x 4096, four
 // slabs of 32 KB 194 us, five 169).
-constexpr int kEpiWarps = 4;
-constexpr int kEpiBytes = 2 * 2048;        // of an epilogue warp: two tiles of 32 rows x 32 features
+// Eight epilogue warps, two for each quarter of the TMEM lanes, which take the tile's 32-row pieces in turn: a piece is a chain of latencies
+// (ViT groups, twelve slabs a tile: four warps were busy for 10,000 of a tile's 12,000 cycles).
+constexpr int kWideAll = 320, kEpiWarps = 8;
+constexpr int kEpiBytes = 2048;            // of an epilogue warp: a tile of 32 rows x 32 features
 template <bool kPair>
-__global__ void __launch_bounds__(kWideThreads, 1)
+__global__ void __launch_bounds__(kWideAll, 1)
 wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmG,
             const __grid_constant__ CUtensorMap tmT, const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ OutParams p) {
   extern __shared__ uint8_t smem_raw[];
@@ -855,9 +858,9 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       }
     }
   } else {
-    const int qw = warp & 3;
+    const int qw = warp & 3, turn = (warp - 2) >> 2;
     const uint32_t lane_base = (uint32_t)(qw * 32) << 16;
-    uint8_t* my = stg + (size_t)(warp - 2) * kEpiBytes;
+    uint8_t* tile_s = stg + (size_t)(warp - 2) * kEpiBytes;
     const uint32_t acc_empty0 = kPair ? cluster_addr(smem_u32(&b->acc_empty[0]), 0) : 0u;
     auto give_back = [&](int buf) {
       tc_fence_before();
@@ -866,7 +869,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         if constexpr (kPair) mbar_arrive_cluster(acc_empty0 + (uint32_t)buf * 8); else mbar_arrive(&b->acc_empty[buf]);
       }
     };
-    int nst = 0, it = 0;
+    int it = 0;
     bool ok = true;
     dep_wait();                          // T is complete; and this kernel is done only after the ones before it
     for (int tile = first_tile; tile < p.ntiles && ok; tile += tile_step, ++it) {
@@ -885,13 +888,9 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
       const bool live = f0 < p.P;
       const int n16 = p.bn / kG;
       bool given = false;
-      for (int g0 = 0; g0 < n16; g0 += 2) {
+      for (int g0 = 2 * turn; g0 < n16; g0 += 4) {
         if (!live || (int64_t)row0 + g0 * kG >= p.N) break;
-        uint8_t* tile_s = my + (nst & 1) * 2048;
-        ++nst;
-        if (lane == 0) tma_store_wait_read<1>();
-        __syncwarp();
-        const bool last = g0 + 2 >= n16 || (int64_t)row0 + (g0 + 2) * kG >= p.N;      // the accumulator's last columns
+        const bool last = g0 + 4 >= n16 || (int64_t)row0 + (g0 + 4) * kG >= p.N;      // the accumulator's last columns
         uint32_t v[2][16];               // features 0..15 and 16..31 of the warp, 32 rows
         tmem_ld_16x32_nowait(tacc + g0 * kG, v[0]);
         tmem_ld_16x32_nowait(tacc + (16u << 16) + g0 * kG, v[1]);
@@ -907,6 +906,8 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           }
           add_mixed(p, (int64_t)row0 + g0 * kG, mine, f0, lane, v);
         }
+        if (elect_one()) tma_store_wait_read<0>();
+        __syncwarp();
         // eight rows (columns 8 j ..) of 32 features are four fragments; transposed they are 8 rows of 64 bytes, whose 16-byte pieces
         // lie where the swizzle puts them
 #pragma unroll
@@ -923,14 +924,14 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
+        if (elect_one()) {
           tma_store_2d(&tmOut, tile_s, f0, row0 + g0 * kG);
           tma_store_commit();
         }
       }
       if (!given) give_back(buf);
     }
-    if (lane == 0) tma_store_wait_all();
+    if (elect_one()) tma_store_wait_all();
     __syncwarp();
   }
 
@@ -1438,16 +1439,17 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   p.nk = (K + 63) / 64;
   p.in_bytes = p.tile_rows * 128;
   p.f_bytes = f_mn ? (cols + 63) / 64 * 8192 : cols * 128;
-  const int least = f_mn ? 16384 : 8192, room = p.f_bytes > least ? p.f_bytes : least;      // two adapters of a tile at once, mostly
-  p.q_max = room / p.f_bytes < 128 / cols ? room / p.f_bytes : 128 / cols;       // two accumulators in half of the columns: two CTAs an SM
-  if (p.q_max > kMaxAd) p.q_max = kMaxAd;
-  p.slot_bytes = p.in_bytes + room;
-  if (p.slot_bytes < 16384) p.slot_bytes = 16384;          // an MMA reads 128 rows of In, loaded or not
   p.csize = 8;
   while (p.csize > 1 && (tiles * p.csize > 2 * sms || 2 * p.csize > p.nk)) p.csize >>= 1;
   // Up to three CTAs an SM, and no more room than for as many as there are: CTAs fill an SM before they go to the next.  The ring takes the
   // parts at the end.
   const int64_t each = (tiles * p.csize * ((rp + 127) / 128) + (c.N <= 2048 ? units : 0) + sms - 1) / sms;
+  // room for the factors of two adapters at once where that leaves as many CTAs their place
+  const int least = f_mn && each <= 2 ? 16384 : 8192, room = p.f_bytes > least ? p.f_bytes : least;
+  p.q_max = room / p.f_bytes < 128 / cols ? room / p.f_bytes : 128 / cols;       // two accumulators in half of the columns: two CTAs an SM
+  if (p.q_max > kMaxAd) p.q_max = kMaxAd;
+  p.slot_bytes = p.in_bytes + room;
+  if (p.slot_bytes < 16384) p.slot_bytes = 16384;          // an MMA reads 128 rows of In, loaded or not
   const int parts = p.tile_rows * (cols + 4) * 4, budget = each <= 1 ? 120 * 1024 : each == 2 ? 96 * 1024 : 72 * 1024;
   p.ns = budget / p.slot_bytes < 3 ? 3 : budget / p.slot_bytes < kMaxStages ? budget / p.slot_bytes : kMaxStages;
   if (p.ns * p.slot_bytes < parts) p.ns = (parts + p.slot_bytes - 1) / p.slot_bytes;
@@ -1533,10 +1535,10 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
   if (pair) {
     AB_CUDA_OK(allow_smem(wide_kernel<true>));
     const int pairs = p.ntiles < sms / 2 ? p.ntiles : sms / 2;
-    return launch_after(wide_kernel<true>, (unsigned)(2 * pairs), (unsigned)kWideThreads, smem, 2, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
+    return launch_after(wide_kernel<true>, (unsigned)(2 * pairs), (unsigned)kWideAll, smem, 2, c.st, tmW, tmIn, tmG, tmT, tmOut, p);
   }
   AB_CUDA_OK(allow_smem(wide_kernel<false>));
-  return launch_after(wide_kernel<false>, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideThreads, smem, 1, c.st, tmW, tmIn, tmG, tmT,
+  return launch_after(wide_kernel<false>, (unsigned)(p.ntiles < sms ? p.ntiles : sms), (unsigned)kWideAll, smem, 1, c.st, tmW, tmIn, tmG, tmT,
                       tmOut, p);
 }
 
