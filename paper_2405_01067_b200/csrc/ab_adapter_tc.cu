@@ -95,44 +95,44 @@ __device__ __forceinline__ void raise(int* abort_any, int* status) {
 }
 
 // ------------------------------------------------------------------------------------------------ what a backward call prepares
-// Blocks 0 .. L-1: the 64-row slabs that have rows of adapter blockIdx.x, ascending: (slab, which of its rows are the adapter's: 32 bits and 32
-// bits, 0).  Blocks behind: T (fp32) cut into pieces, eight values a thread.  Reads the call's inputs alone, so it runs beside the
-// kernel before it.
-constexpr int kPrepThreads = 512;
-__global__ void __launch_bounds__(kPrepThreads)
-prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint4* __restrict__ list, int* __restrict__ count, int nslab, const float* __restrict__ T,
-            bf16* __restrict__ P, int r, int rp, int first, int* status) {
-  __shared__ int warp_cnt[kPrepThreads / 32];
-  if (first) dep_wait();
-  dep_launch();
-  if (first && blockIdx.x == 0 && threadIdx.x == 0) *status = AB_OK;
-  if ((int)blockIdx.x >= L) {
-    const int64_t step = (int64_t)(gridDim.x - L) * kPrepThreads;
+// CTAs 0 .. L-1: the 64-row slabs that have rows of adapter `cta`, ascending: (slab, which of its rows are the adapter's: 32 bits and 32 bits,
+// 0).  CTAs behind: T (fp32) cut into pieces, eight values a thread.  Reads the call's inputs alone: it runs beside the projection, in
+// one launch with it (a launch of its own found no room before the kernel in front of it had ended: 20 us for the ViT groups).
+struct PrepParams {
+  uint4* list; int* count; int nslab;
+  const float* T; bf16* P;
+  int ctas;                                 // all of them; 0: nothing to prepare
+};
+template <int kWarps>
+__device__ __forceinline__ void prep_body(const PrepParams& q, const int* __restrict__ ids, int64_t N, int L, int r, int rp, int cta, int tid,
+                                          int* warp_cnt) {
+  if (cta >= L) {
+    const int64_t step = (int64_t)(q.ctas - L) * 32 * kWarps;
     const int oct = rp / 8;
-    for (int64_t i = (int64_t)(blockIdx.x - L) * kPrepThreads + threadIdx.x; i < N * oct; i += step) {
+    for (int64_t i = (int64_t)(cta - L) * 32 * kWarps + tid; i < N * oct; i += step) {
       const int64_t row = i / oct;
       const int k = (int)(i - row * oct) * 8;
       float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (k < r) {
-        const float4 t0 = *reinterpret_cast<const float4*>(T + row * r + k), t1 = *reinterpret_cast<const float4*>(T + row * r + k + 4);
+        const float4 t0 = *reinterpret_cast<const float4*>(q.T + row * r + k), t1 = *reinterpret_cast<const float4*>(q.T + row * r + k + 4);
         v[0] = t0.x; v[1] = t0.y; v[2] = t0.z; v[3] = t0.w; v[4] = t1.x; v[5] = t1.y; v[6] = t1.z; v[7] = t1.w;
       }
-      put_pieces(P + row * 3 * rp + k, rp, v);
+      put_pieces(q.P + row * 3 * rp + k, rp, v);
     }
     fence_proxy_async_all();
     return;
   }
-  const int a = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint4* mine = list + (int64_t)a * nslab;
+  const int lane = tid & 31, warp = tid >> 5;
+  uint4* mine = q.list + (int64_t)cta * q.nslab;
   int at = 0;
-  for (int s0 = 0; s0 < nslab; s0 += kPrepThreads) {
+  for (int s0 = 0; s0 < q.nslab; s0 += 32 * kWarps) {
     // a warp looks at 32 slabs, lane e keeps what slab e is
     unsigned lo = 0u, hi = 0u;
     const int w0 = s0 + warp * 32;
-#pragma unroll 8
+#pragma unroll 16
     for (int e = 0; e < 32; ++e) {
       const int64_t row = (int64_t)(w0 + e) * 64 + lane;
-      const bool x = row < N && ids[row] == a, y = row + 32 < N && ids[row + 32] == a;
+      const bool x = row < N && ids[row] == cta, y = row + 32 < N && ids[row + 32] == cta;
       const unsigned vx = __ballot_sync(0xffffffffu, x), vy = __ballot_sync(0xffffffffu, y);
       if (lane == e) { lo = vx; hi = vy; }
     }
@@ -141,8 +141,7 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint4* __restrict__ l
     if (lane == 0) warp_cnt[warp] = __popc(vote);
     __syncthreads();
     int ahead = 0, sum = 0;
-#pragma unroll
-    for (int w = 0; w < kPrepThreads / 32; ++w) {
+    for (int w = 0; w < kWarps; ++w) {
       const int c = warp_cnt[w];
       ahead += w < warp ? c : 0;
       sum += c;
@@ -151,10 +150,18 @@ prep_kernel(const int* __restrict__ ids, int64_t N, int L, uint4* __restrict__ l
     at += sum;
     __syncthreads();
   }
-  if (threadIdx.x == 0) count[a] = at;
-  // The kernel is done only after the one before it.  One block waits: were it all of them, those that find no room beside that kernel
-  // would not begin before it ends.
-  if (!first && blockIdx.x == 0) dep_wait();
+  if (tid == 0) q.count[cta] = at;
+}
+
+// By itself where no projection is launched by tiles.
+constexpr int kPrepThreads = 512;
+__global__ void __launch_bounds__(kPrepThreads)
+prep_kernel(const __grid_constant__ PrepParams q, const int* __restrict__ ids, int64_t N, int L, int r, int rp, int first, int* status) {
+  __shared__ int warp_cnt[kPrepThreads / 32];
+  dep_wait();
+  dep_launch();
+  if (first && blockIdx.x == 0 && threadIdx.x == 0) *status = AB_OK;
+  prep_body<kPrepThreads / 32>(q, ids, N, L, r, rp, blockIdx.x, threadIdx.x, warp_cnt);
 }
 
 // ------------------------------------------------------------------------------------------------ T of rows in mixed groups
@@ -197,7 +204,8 @@ struct ProjParams {
   int first;                                // the call's first kernel
   int* status;
   // project_tc_kernel
-  int tile_ctas;                            // CTAs that have tiles
+  int prep_ctas, tile_ctas;                 // CTAs that prepare, whole clusters (they come first: lists are chains), and that have tiles
+  PrepParams prep;
   int nk, csize, ns, slot_bytes, in_bytes, f_bytes, q_max, tmem_cols;
 };
 
@@ -338,7 +346,7 @@ struct ProjBars {
 };
 
 template <int kChunks>                    // up to 16 kChunks values of r a CTA
-__global__ void __launch_bounds__(kProjTcThreads)
+__global__ void __launch_bounds__(kProjTcThreads, kChunks <= 4 ? 3 : 1)
 project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmF, const __grid_constant__ ProjParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -347,14 +355,21 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
   if (p.first) dep_wait();
   dep_launch();
   if (p.first && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = AB_OK;
-  if ((int)blockIdx.x >= p.tile_ctas) {    // behind the tiles: rows that go one by one
-    if (blockIdx.y == 0 && (int64_t)(blockIdx.x - p.tile_ctas) * p.unit < p.N)
-      rows_body<kProjTcThreads / 32>(p, blockIdx.x - p.tile_ctas, 0, 1, threadIdx.x, reinterpret_cast<float(*)[32][8]>(ring));
+  const int cta = (int)blockIdx.x - p.prep_ctas;
+  if (cta < 0 || cta >= p.tile_ctas) {
+    if (blockIdx.y == 0) {
+      if (cta < 0) {
+        if ((int)blockIdx.x < p.prep.ctas)
+          prep_body<kProjTcThreads / 32>(p.prep, p.ids, p.N, p.L, p.r, p.rp, blockIdx.x, threadIdx.x, reinterpret_cast<int*>(ring));
+      } else if ((int64_t)(cta - p.tile_ctas) * p.unit < p.N) {      // behind the tiles: rows that go one by one
+        rows_body<kProjTcThreads / 32>(p, cta - p.tile_ctas, 0, 1, threadIdx.x, reinterpret_cast<float(*)[32][8]>(ring));
+      }
+    }
     fence_proxy_async_all();
     if (!p.first) dep_wait();
     return;
   }
-  const int tile = (int)blockIdx.x / p.csize, rank = (int)blockIdx.x - tile * p.csize;
+  const int tile = cta / p.csize, rank = cta - tile * p.csize;
   const int64_t row0 = (int64_t)tile * p.tile_rows;
   const int kc0 = (int)blockIdx.y * 128, cols = p.rp - kc0 < 128 ? p.rp - kc0 : 128;
   const int per = (p.nk + p.csize - 1) / p.csize, i0 = rank * per, i1 = i0 + per < p.nk ? i0 + per : p.nk;
@@ -1397,6 +1412,12 @@ adapter_grad_tc_kernel(const __grid_constant__ CUtensorMap tmAct0, const __grid_
 }
 
 // ------------------------------------------------------------------------------------------------ host
+// Lets a kernel of little shared memory begin on SMs whose memory is set up for one that takes all of it.
+template <typename K>
+cudaError_t beside_large(K* kernel) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+}
+
 int pad16(int r) { return (r + 15) / 16 * 16; }
 int pow2_cols(int c) { int v = 32; while (v < c) v <<= 1; return v; }
 
@@ -1415,7 +1436,7 @@ int stack_map(CUtensorMap* m, const AdapterCall& c, const void* F, int rows, int
 
 // T = s F In of all rows (two launches, or one for few rows); `first`: nothing of the call was launched before
 int launch_project(const AdapterCall& c, const void* In, int K, const void* F, int64_t strideF, bool f_mn, float* T, bool want_T, int out_width, bf16* P,
-                   bool first, int* status) {
+                   bool first, PrepParams* prep, int* status) {
   const int sms = sm_count();
   if (sms <= 0) return AB_ERR_CUDA;
   ProjParams p;
@@ -1433,6 +1454,7 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   const int64_t units = (c.N + p.unit - 1) / p.unit;
   if (p.all_rows) {
     const int ky = f_mn ? 1 : (rp + kRowsThreads / 32 - 1) / (kRowsThreads / 32);
+    AB_CUDA_OK(beside_large(rows_kernel));
     return launch_after(rows_kernel, dim3((unsigned)units, (unsigned)ky), (unsigned)kRowsThreads, 0, 1, c.st, p);
   }
   const int cols = rp < 128 ? rp : 128;
@@ -1458,7 +1480,12 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.tile_rows));
   AB_TRY(stack_map(&tmF, c, F, f_mn ? K : c.r, f_mn ? c.r : K, strideF, f_mn ? 64 : cols));
   p.tile_ctas = (int)(tiles * p.csize);
-  const int64_t ctas = tiles * p.csize + (units + p.csize - 1) / p.csize * p.csize;
+  if (prep) {                               // taken along
+    p.prep = *prep;
+    prep->ctas = 0;
+  }
+  p.prep_ctas = (p.prep.ctas + p.csize - 1) / p.csize * p.csize;
+  const int64_t ctas = p.prep_ctas + tiles * p.csize + (units + p.csize - 1) / p.csize * p.csize;
   if (ctas > 0x7fffffffll) return AB_ERR_UNSUPPORTED;
   size_t smem = 1024 + (size_t)p.ns * p.slot_bytes + sizeof(ProjBars);
   if (smem < (size_t)budget) smem = budget;
@@ -1639,30 +1666,34 @@ size_t adapter_tc_ws(int64_t N, int m, int n, int r, int L) { return tc_ws(nullp
 int adapter_tc_forward(const AdapterCall& c, void* y, float* T_save, void* ws) {
   const TcWs w = tc_ws(ws, c.N, c.m, c.n, c.r, c.L);
   float* T = T_save ? T_save : w.T;
-  AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, T, T_save != nullptr, c.m, w.TP, true, w.status));
+  AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, T, T_save != nullptr, c.m, w.TP, true, nullptr, w.status));
   return launch_out(c, c.x, c.n, false, c.A, c.strideA, y, c.m, T, w.TP, w.status);
 }
 
 int adapter_tc_backward(const AdapterCall& c, const void* dY, const float* T_saved, void* dX, float* dA, float* dB, void* ws) {
   const TcWs w = tc_ws(ws, c.N, c.m, c.n, c.r, c.L);
   bool first = true;
+  PrepParams prep = {};
+  if (dA || dB) {
+    const int64_t values = dA && T_saved ? c.N * (pad16(c.r) / 8) : 0;
+    const int64_t blocks = (values + 1023) / 1024;
+    prep = PrepParams{w.list, w.count, w.nslab, T_saved, w.TP, c.L + (int)(blocks < 444 ? blocks : 444)};
+  }
   if (dX || dB) {
-    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, false, c.n, w.UP, first, w.status));
+    AB_TRY(launch_project(c, dY, c.m, c.A, c.strideA, true, w.U, false, c.n, w.UP, first, &prep, w.status));
     first = false;
   }
   if (dA && !T_saved) {
-    AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, false, c.m, w.TP, first, w.status));
+    AB_TRY(launch_project(c, c.x, c.n, c.B, c.strideB, false, w.T, false, c.m, w.TP, first, &prep, w.status));
     first = false;
   }
-  if (dX) AB_TRY(launch_out(c, dY, c.m, true, c.B, c.strideB, dX, c.n, w.U, w.UP, w.status));
-  if (dA || dB) {
-    const int64_t rows = dA && T_saved ? c.N : 0;
-    int64_t blocks = (rows * (pad16(c.r) / 8) + kPrepThreads - 1) / kPrepThreads;
-    if (blocks > 1024) blocks = 1024;
-    AB_TRY(launch_after(prep_kernel, (unsigned)(c.L + blocks), (unsigned)kPrepThreads, 0, 1, c.st, c.ids, c.N, c.L, w.list, w.count, w.nslab, T_saved, w.TP,
-                        c.r, pad16(c.r), first ? 1 : 0, w.status));
-    AB_TRY(launch_grads(c, dY, dA, dB, w, !dX));
+  if (prep.ctas > 0) {                      // no projection took it along
+    AB_CUDA_OK(beside_large(prep_kernel));
+    AB_TRY(launch_after(prep_kernel, (unsigned)prep.ctas, (unsigned)kPrepThreads, 0, 1, c.st, prep, c.ids, c.N, c.L, c.r, pad16(c.r), first ? 1 : 0,
+                        w.status));
   }
+  if (dX) AB_TRY(launch_out(c, dY, c.m, true, c.B, c.strideB, dX, c.n, w.U, w.UP, w.status));
+  if (dA || dB) AB_TRY(launch_grads(c, dY, dA, dB, w, !dX));
   return AB_OK;
 }
 
