@@ -256,12 +256,12 @@ list_rows_kernel(const int* __restrict__ ids, int64_t N, int L, int* __restrict_
 // has 64 values of f and 32 of k of one adapter; rows in their order, 64 at a time in fp32, those sums in fp64: a long sum loses
 // nothing that fp32 shows.
 constexpr int kGF = 64, kGK = 32, kGR = 64;
-struct GradSide { const void* In; int P, tiles; const float* S; float* D; int64_t strideD, d_f, d_k; };
+struct GradSide { const void* In; int P, tiles; const float* S; float* D; int64_t strideD, d_f, d_k, slice; };      // slice: from slice to slice
 struct GradSides { GradSide side[2]; };
 template <typename TI>
 __global__ void __launch_bounds__(256)
 adapter_grad_kernel(const __grid_constant__ GradSides sides, int r, const int* __restrict__ order, const int64_t* __restrict__ start,
-                    const int64_t* __restrict__ count) {
+                    const int64_t* __restrict__ count, int slices) {
   __shared__ float Is[kGR][kGF];
   __shared__ float4 Ss[kGR][kGK / 4];
   __shared__ int rows[kGR];
@@ -271,10 +271,12 @@ adapter_grad_kernel(const __grid_constant__ GradSides sides, int r, const int* _
   const GradSide& w = sides.side[second];
   const TI* In = static_cast<const TI*>(w.In);
   const int P = w.P;
-  const int f0 = ((int)blockIdx.x - (second ? sides.side[0].tiles : 0)) * kGF, k0 = blockIdx.y * kGK, a = blockIdx.z;
+  const int f0 = ((int)blockIdx.x - (second ? sides.side[0].tiles : 0)) * kGF, k0 = blockIdx.y * kGK, a = (int)blockIdx.z / slices, part = (int)blockIdx.z - a * slices;
   const int f = threadIdx.x % kGF, kq = threadIdx.x / kGF;      // this thread: column f, values 8 kq .. 8 kq + 7
-  const int64_t n = count[a];
-  const int* mine = order + start[a];
+  // this slice's rows, whole blocks of kGR
+  const int64_t all = count[a], per = ((all + slices - 1) / slices + kGR - 1) / kGR * kGR, from = part * per < all ? part * per : all;
+  const int64_t n = all - from < per ? all - from : per;
+  const int* mine = order + start[a] + from;
   double acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0;
@@ -308,10 +310,22 @@ adapter_grad_kernel(const __grid_constant__ GradSides sides, int r, const int* _
     for (int e = 0; e < 8; ++e) acc[e] += (double)v[e];
   }
   if (f0 + f >= P) return;
-  float* d = w.D + a * w.strideD + (f0 + f) * w.d_f;
+  float* d = w.D + part * w.slice + a * w.strideD + (f0 + f) * w.d_f;
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     if (k0 + 8 * kq + e < r) d[(k0 + 8 * kq + e) * w.d_k] = (float)acc[e];
+}
+
+// out[i] = sum over the slices, in their order
+__global__ void __launch_bounds__(256)
+add_slices_kernel(const float* __restrict__ part, float* __restrict__ out, int64_t count, int slices) {
+  tc::dep_wait();
+  tc::dep_launch();
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= count) return;
+  float v = part[i];
+  for (int s = 1; s < slices; ++s) v += part[s * count + i];
+  out[i] = v;
 }
 
 typedef AdapterCall Call;
@@ -336,7 +350,16 @@ int base_slices(int64_t N, int P, int K) {
 bool base_small(const Call& c, int P, int K) { return c.dt == AB_F32 && gemm_small_pays(c.N, P, K); }
 
 // Workspace of the general path: status word, T, U, the shared product, the adapters' rows
-struct GeneralWs { int* status; float *T, *U, *base; int* order; int64_t *start, *count; size_t bytes; };
+// Slices of the rows where the gradients' tiles are few (4006 rows of one adapter, rank 4, 208 x 656: 15 blocks took 250 us)
+int grad_slices(int64_t N, int m, int n, int r, int L) {
+  const int sms = sm_count() > 0 ? sm_count() : 148;
+  const int64_t blocks = (int64_t)((m + kGF - 1) / kGF + (n + kGF - 1) / kGF) * ((r + kGK - 1) / kGK) * L;
+  int64_t s = 2 * sms / blocks;
+  if (s > N / (2 * kGR)) s = N / (2 * kGR);
+  return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+}
+
+struct GeneralWs { int* status; float *T, *U, *base; int* order; int64_t *start, *count; float *pA, *pB; int slices; size_t bytes; };
 GeneralWs general_ws(void* ws, int64_t N, int m, int n, int r, int L, int dt) {
   Arena ar(ws, 0);
   GeneralWs w;
@@ -350,6 +373,9 @@ GeneralWs general_ws(void* ws, int64_t N, int m, int n, int r, int L, int dt) {
   w.order = ar.take_n<int>((size_t)N);
   w.start = ar.take_n<int64_t>((size_t)L);
   w.count = ar.take_n<int64_t>((size_t)L);
+  w.slices = grad_slices(N, m, n, r, L);
+  w.pA = w.slices > 1 ? ar.take_n<float>((size_t)w.slices * L * m * r) : nullptr;
+  w.pB = w.slices > 1 ? ar.take_n<float>((size_t)w.slices * L * n * r) : nullptr;
   w.bytes = align_up(ar.used, 256);
   return w;
 }
@@ -412,20 +438,25 @@ int shared_and_delta(const Call& c, const void* In, int K, bool w_mn, const floa
 }
 
 int grads(const Call& c, const GeneralWs& w, const void* dY, const float* T, float* dA, float* dB) {
+  const int64_t ea = (int64_t)c.L * c.m * c.r, eb = (int64_t)c.L * c.n * c.r;
   GradSides s;
   memset(&s, 0, sizeof(s));
   int n = 0;
-  if (dA) s.side[n++] = GradSide{dY, c.m, (c.m + kGF - 1) / kGF, T, dA, (int64_t)c.m * c.r, c.r, 1};
-  if (dB) s.side[n++] = GradSide{c.x, c.n, (c.n + kGF - 1) / kGF, w.U, dB, (int64_t)c.r * c.n, 1, c.n};
+  if (dA) s.side[n++] = GradSide{dY, c.m, (c.m + kGF - 1) / kGF, T, w.slices > 1 ? w.pA : dA, (int64_t)c.m * c.r, c.r, 1, ea};
+  if (dB) s.side[n++] = GradSide{c.x, c.n, (c.n + kGF - 1) / kGF, w.U, w.slices > 1 ? w.pB : dB, (int64_t)c.r * c.n, 1, c.n, eb};
   const unsigned tiles = (unsigned)(s.side[0].tiles + s.side[1].tiles);
-  for (int a0 = 0; a0 < c.L; a0 += 65535) {
-    const dim3 grid(tiles, (unsigned)((c.r + kGK - 1) / kGK), (unsigned)(c.L - a0 < 65535 ? c.L - a0 : 65535));
+  const int step = 65535 / w.slices;          // adapters of a launch
+  for (int a0 = 0; a0 < c.L; a0 += step) {
+    const dim3 grid(tiles, (unsigned)((c.r + kGK - 1) / kGK), (unsigned)((c.L - a0 < step ? c.L - a0 : step) * w.slices));
     const int* order = w.order;
     const int64_t *start = w.start + a0, *count = w.count + a0;
-    if (c.dt == AB_F32) AB_TRY(launch_after(adapter_grad_kernel<float>, grid, 256u, 0, 1, c.st, s, c.r, order, start, count));
-    else AB_TRY(launch_after(adapter_grad_kernel<bf16>, grid, 256u, 0, 1, c.st, s, c.r, order, start, count));
-    for (int i = 0; i < n; ++i) s.side[i].D += 65535 * s.side[i].strideD;
+    if (c.dt == AB_F32) AB_TRY(launch_after(adapter_grad_kernel<float>, grid, 256u, 0, 1, c.st, s, c.r, order, start, count, w.slices));
+    else AB_TRY(launch_after(adapter_grad_kernel<bf16>, grid, 256u, 0, 1, c.st, s, c.r, order, start, count, w.slices));
+    for (int i = 0; i < n; ++i) s.side[i].D += step * s.side[i].strideD;
   }
+  if (w.slices == 1) return AB_OK;
+  if (dA) AB_TRY(launch_after(add_slices_kernel, (unsigned)((ea + 255) / 256), 256u, 0, 1, c.st, (const float*)w.pA, dA, ea, w.slices));
+  if (dB) AB_TRY(launch_after(add_slices_kernel, (unsigned)((eb + 255) / 256), 256u, 0, 1, c.st, (const float*)w.pB, dB, eb, w.slices));
   return AB_OK;
 }
 

@@ -240,6 +240,31 @@ __device__ __forceinline__ void rows_body(const ProjParams& p, int64_t unit, int
       if (a < 0) {
         if (part == 0) for (int k = tid; k < p.rp; k += 32 * kWarps) put_T(p, row, k, 0.f);
       } else if (!p.f_mn) {
+        // short rows leave little to load for a value: four values at a time (rank 128, rows of 160: 22 rounds of a trip to L2 each)
+        if (p.K <= 1024 && p.r >= 4 * kWarps) {
+          for (int k = (part * kWarps + warp) * 4; k < p.rp; k += parts * kWarps * 4) {
+            const uint4* f[4];
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = reinterpret_cast<const uint4*>(p.F + a * p.strideF + (int64_t)(k + e < p.r ? k + e : p.r - 1) * p.K);
+#pragma unroll 2
+            for (int j = lane; j < p.K / 8; j += 32) {
+              const uint4 w = x[j];
+              const uint32_t xs[4] = {w.x, w.y, w.z, w.w};
+              float t[8];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) { t[2 * i] = __uint_as_float(xs[i] << 16); t[2 * i + 1] = __uint_as_float(xs[i] & 0xffff0000u); }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) dot8(f[e][j], t, v[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+#pragma unroll
+              for (int o = 16; o > 0; o >>= 1) v[e] += __shfl_xor_sync(0xffffffffu, v[e], o);
+              if (lane == 0) put_T(p, row, k + e, k + e < p.r ? s * v[e] : 0.f);
+            }
+          }
+        } else
         for (int k = part * kWarps + warp; k < p.rp; k += parts * kWarps) {
           float v = 0.f;
           if (k < p.r) {
@@ -1513,9 +1538,13 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
   if (mn) AB_TRY(make_tensor_map_2d(&tmW, c.W, false, K, P, P, 64, 64));
   else AB_TRY(make_tensor_map_2d(&tmW, c.W, false, P, K, K, 64, 128));
   if (few_rows(c.N, P)) {
+    // As many CTAs as there are SMs, by parts of the reduction, and where that is short by fewer rows a tile (127 rows of 25 adapters, rank
+    // 128, 160 x 232: with 64 rows a CTA 13 pieces of G came one after the other)
     p.bn = c.N <= 64 ? (int)((c.N + 15) / 16 * 16) : 64;
-    const int64_t tt = (c.N + p.bn - 1) / p.bn;
     p.csize = 8;
+    while (p.csize > 1 && 2 * p.csize > p.nk) p.csize >>= 1;
+    while (p.bn % 32 == 0 && p.nft * ((c.N + p.bn / 2 - 1) / (p.bn / 2)) * p.csize <= sms) p.bn /= 2;
+    const int64_t tt = (c.N + p.bn - 1) / p.bn;
     while (p.csize > 1 && (p.nft * tt * p.csize > sms || 2 * p.csize > p.nk)) p.csize >>= 1;
     p.share = ((p.bn + p.csize - 1) / p.csize + 3) / 4 * 4;
     p.slot_bytes = kABytes + p.bn * 128;

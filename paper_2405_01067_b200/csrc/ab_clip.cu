@@ -16,7 +16,9 @@ constexpr int kClipThreads = 512;
 // Tensors of one launch: their records are kernel arguments, so nothing is copied in front of the launch and a captured call is whole.  A
 // short table where it is enough: arguments are copied at every launch.
 constexpr int kClipShort = 160, kClipLong = 1000;
-constexpr int kClipChunk = 32768;           // bytes of one chunk
+// Bytes of a chunk: the longest with which every CTA still gets three.  Long ones have fewer beginnings and ends (1 GB of bf16: chunks of
+// 32 KB 597 us, 128 KB 538), short ones spread evenly over the CTAs (the 144 factors of ViT-B/16: 16 KB 100 us).
+constexpr int kChunkShort = 16384, kChunkLong = 131072;
 constexpr int kClipMaxCtas = 148 * 4;
 
 struct ClipRec { const void* g; void* out; int64_t count; };
@@ -24,7 +26,7 @@ template <int kCap>
 struct ClipTable {
   ClipRec rec[kCap];
   int first[kCap + 1];                      // chunk index at which each tensor begins
-  int tensors;
+  int tensors, chunk;                       // chunk: bytes
 };
 
 // The square of a value in fp32 overflows above 1.8e19 and vanishes below 1e-23: four squares are added in fp32 where their sum says that
@@ -82,7 +84,7 @@ __device__ __forceinline__ int find_tensor(const ClipTable<kCap>& t, int q) {
 // last few values of a tensor go by 16-byte loads wherever it starts.
 template <typename T, int kCap>
 __device__ __forceinline__ void chunk_range(const ClipTable<kCap>& t, int q, int i, int64_t& from, int64_t& to) {
-  const int64_t per = kClipChunk / (int64_t)sizeof(T), count = t.rec[i].count;
+  const int64_t per = t.chunk / (int64_t)sizeof(T), count = t.rec[i].count;
   const int64_t skew = (int64_t)((reinterpret_cast<uintptr_t>(t.rec[i].g) & 15) / sizeof(T));     // values past a 16-byte boundary
   const int64_t c = q - t.first[i];
   from = c == 0 ? 0 : c * per - skew;
@@ -102,6 +104,70 @@ __device__ __forceinline__ double block_sum(double v) {
   return s;
 }
 
+// Adds the squares of chunk q.
+template <typename T, int kCap>
+__device__ __forceinline__ void chunk_squares(const ClipTable<kCap>& t, int q, double& acc) {
+  const int i = find_tensor(t, q);
+  int64_t from, to;
+  chunk_range<T>(t, q, i, from, to);
+  const T* g = static_cast<const T*>(t.rec[i].g);
+  // up to the first 16-byte boundary, whole 16-byte groups, the rest
+  int64_t head = ((16 - (reinterpret_cast<uintptr_t>(g + from) & 15)) & 15) / sizeof(T);
+  if (head > to - from) head = to - from;
+  const int groups = (int)((to - from - head) / Vec<T>::n);
+  const int64_t tail = from + head + (int64_t)groups * Vec<T>::n;
+  const uint4* v = reinterpret_cast<const uint4*>(g + from + head);
+  if (threadIdx.x < head) { const double x = to_f32(g[from + threadIdx.x]); acc += x * x; }
+  if (tail + threadIdx.x < to) { const double x = to_f32(g[tail + threadIdx.x]); acc += x * x; }
+  for (int k = threadIdx.x; k < groups; k += 8 * kClipThreads) {
+    uint4 u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (k + e * kClipThreads < groups) u[e] = v[k + e * kClipThreads];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (k + e * kClipThreads < groups) Vec<T>::squares(u[e], acc);
+  }
+}
+
+// out = g c over chunk q.
+template <typename T, int kCap>
+__device__ __forceinline__ void chunk_scaled(const ClipTable<kCap>& t, int q, float c) {
+  const int i = find_tensor(t, q);
+  int64_t from, to;
+  chunk_range<T>(t, q, i, from, to);
+  const T* g = static_cast<const T*>(t.rec[i].g);
+  T* out = static_cast<T*>(t.rec[i].out);
+  if (c == 1.f && g == out) return;                       // nothing to do where it lies
+  if (((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(out)) & 15) != 0) {
+    for (int64_t k = from + threadIdx.x; k < to; k += kClipThreads) from_f32(out[k], c == 1.f ? to_f32(g[k]) : to_f32(g[k]) * c);
+    return;
+  }
+  int64_t head = ((16 - (reinterpret_cast<uintptr_t>(g + from) & 15)) & 15) / sizeof(T);
+  if (head > to - from) head = to - from;
+  const int groups = (int)((to - from - head) / Vec<T>::n);
+  const int64_t tail = from + head + (int64_t)groups * Vec<T>::n;
+  const uint4* v = reinterpret_cast<const uint4*>(g + from + head);
+  uint4* w = reinterpret_cast<uint4*>(out + from + head);
+  if (threadIdx.x < head) from_f32(out[from + threadIdx.x], to_f32(g[from + threadIdx.x]) * c);
+  if (tail + threadIdx.x < to) from_f32(out[tail + threadIdx.x], to_f32(g[tail + threadIdx.x]) * c);
+  for (int k = threadIdx.x; k < groups; k += 8 * kClipThreads) {
+    uint4 u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (k + e * kClipThreads < groups) u[e] = v[k + e * kClipThreads];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (k + e * kClipThreads < groups) __stcs(w + k + e * kClipThreads, Vec<T>::scaled(u[e], c));
+  }
+}
+
+// The factor; a norm that is infinite or NaN scales nothing: the caller sees it and can drop the step.
+__device__ __forceinline__ float clip_factor(double norm, float max_norm) {
+  const double big = max_norm;
+  return norm > big && norm <= 1.7976931348623157e308 ? (float)(big / norm) : 1.f;
+}
+
 // part[blockIdx.x]: the sum of the squares of this CTA's chunks (q = blockIdx.x, + grid, ...), on top of what an earlier launch left there
 template <typename T, int kCap>
 __global__ void __launch_bounds__(kClipThreads)
@@ -109,28 +175,7 @@ clip_norm_kernel(const __grid_constant__ ClipTable<kCap> t, int chunks, double* 
   tc::dep_wait();
   tc::dep_launch();
   double acc = 0.0;
-  for (int q = blockIdx.x; q < chunks; q += gridDim.x) {
-    const int i = find_tensor(t, q);
-    int64_t from, to;
-    chunk_range<T>(t, q, i, from, to);
-    const T* g = static_cast<const T*>(t.rec[i].g);
-    // up to the first 16-byte boundary, whole 16-byte groups, the rest
-    int64_t head = ((16 - (reinterpret_cast<uintptr_t>(g + from) & 15)) & 15) / sizeof(T);
-    if (head > to - from) head = to - from;
-    const int64_t groups = (to - from - head) / Vec<T>::n, tail = from + head + groups * Vec<T>::n;
-    const uint4* v = reinterpret_cast<const uint4*>(g + from + head);
-    if (threadIdx.x < head) { const double x = to_f32(g[from + threadIdx.x]); acc += x * x; }
-    if (tail + threadIdx.x < to) { const double x = to_f32(g[tail + threadIdx.x]); acc += x * x; }
-    for (int64_t k = threadIdx.x; k < groups; k += 4 * kClipThreads) {
-      uint4 u[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (k + e * kClipThreads < groups) u[e] = v[k + e * kClipThreads];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (k + e * kClipThreads < groups) Vec<T>::squares(u[e], acc);
-    }
-  }
+  for (int q = blockIdx.x; q < chunks; q += gridDim.x) chunk_squares<T>(t, q, acc);
   const double s = block_sum(acc);
   if (threadIdx.x == 0) part[blockIdx.x] = add ? part[blockIdx.x] + s : s;
 }
@@ -144,39 +189,10 @@ clip_scale_kernel(const __grid_constant__ ClipTable<kCap> t, int chunks, const d
   double acc = 0.0;
   for (int p = threadIdx.x; p < parts; p += kClipThreads) acc += __ldcg(part + p);
   const double norm = sqrt(block_sum(acc));
-  // a norm that is infinite or NaN scales nothing: the caller sees it and can drop the step
-  const double big = max_norm;
-  const float c = norm > big && norm <= 1.7976931348623157e308 ? (float)(big / norm) : 1.f;
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   if (!write) return;
-  for (int b = blockIdx.x; b < chunks; b += gridDim.x) {
-    const int q = chunks - 1 - b, i = find_tensor(t, q);
-    int64_t from, to;
-    chunk_range<T>(t, q, i, from, to);
-    const T* g = static_cast<const T*>(t.rec[i].g);
-    T* out = static_cast<T*>(t.rec[i].out);
-    if (c == 1.f && g == out) continue;                     // nothing to do where it lies
-    if (((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(out)) & 15) != 0) {
-      for (int64_t k = from + threadIdx.x; k < to; k += kClipThreads) from_f32(out[k], c == 1.f ? to_f32(g[k]) : to_f32(g[k]) * c);
-      continue;
-    }
-    int64_t head = ((16 - (reinterpret_cast<uintptr_t>(g + from) & 15)) & 15) / sizeof(T);
-    if (head > to - from) head = to - from;
-    const int64_t groups = (to - from - head) / Vec<T>::n, tail = from + head + groups * Vec<T>::n;
-    const uint4* v = reinterpret_cast<const uint4*>(g + from + head);
-    uint4* w = reinterpret_cast<uint4*>(out + from + head);
-    if (threadIdx.x < head) from_f32(out[from + threadIdx.x], to_f32(g[from + threadIdx.x]) * c);
-    if (tail + threadIdx.x < to) from_f32(out[tail + threadIdx.x], to_f32(g[tail + threadIdx.x]) * c);
-    for (int64_t k = threadIdx.x; k < groups; k += 4 * kClipThreads) {
-      uint4 u[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (k + e * kClipThreads < groups) u[e] = v[k + e * kClipThreads];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (k + e * kClipThreads < groups) __stcs(w + k + e * kClipThreads, Vec<T>::scaled(u[e], c));
-    }
-  }
+  const float c = clip_factor(norm, max_norm);
+  for (int b = blockIdx.x; b < chunks; b += gridDim.x) chunk_scaled<T>(t, chunks - 1 - b, c);
 }
 
 // A table from tensor i on; returns the first tensor that is not in it.
@@ -188,7 +204,7 @@ int fill_table(ClipTable<kCap>& t, const ab_clip_desc* d, int L, int i, int dt, 
   for (; i < L && t.tensors < kCap; ++i) {
     if (d[i].count == 0) continue;
     const int64_t skew = (int64_t)(reinterpret_cast<uintptr_t>(d[i].grad) & 15);
-    const int64_t n = (d[i].count * esz + skew + kClipChunk - 1) / kClipChunk;
+    const int64_t n = (d[i].count * esz + skew + t.chunk - 1) / t.chunk;
     if (t.tensors > 0 && q + n > 0x7fffffffll) break;
     t.rec[t.tensors] = ClipRec{d[i].grad, d[i].out, d[i].count};
     t.first[t.tensors++] = (int)q;
@@ -208,6 +224,10 @@ template <typename T, int kCap>
 int clip_run(const ab_clip_desc* d, int L, float max_norm, float* norm_out, double* part, int dt, bool write, cudaStream_t st) {
   ClipTable<kCap> t;
   int chunks, parts = 0, next;
+  int64_t bytes = 0;
+  for (int i = 0; i < L; ++i) bytes += d[i].count * (int64_t)dtype_size(dt);
+  t.chunk = kChunkShort;
+  while (t.chunk < kChunkLong && bytes / (2 * t.chunk) >= 3 * clip_grid(kClipMaxCtas)) t.chunk *= 2;
   for (int i = 0; i < L || i == 0; i = next) {
     next = fill_table(t, d, L, i, dt, &chunks);
     // the first launch sets the sums that later ones add to: where there are later ones it has all the CTAs that there can be

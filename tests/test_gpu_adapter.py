@@ -399,3 +399,18 @@ def test_bad_entries_among_many_rows():
         assert ab.workspace_status(ws) == ab.AB_ERR_INVALID_ARG
         y2, _ = ab.ab_adapter_forward(x, W, A, B, right, scale=s, ws=ws)
         assert ab.workspace_status(ws) == ab.AB_OK and torch.equal(y, y2)
+
+
+@pytest.mark.parametrize("dtype,N,m,n,r,L,kind", [(BF16, 1500, 72, 100, 4, 1, "one"), (F32, 700, 65, 130, 5, 2, "mixed"), (BF16, 2000, 40, 33, 12, 3, "runs"),
+                                                  (F32, 3000, 100, 60, 3, 1, "single"), (BF16, 127, 232, 160, 128, 25, "runs"),
+                                                  (BF16, 120, 216, 264, 200, 30, "single"), (F32, 300, 40, 1600, 8, 4, "mixed")])
+def test_few_tiles_many_rows(dtype, N, m, n, r, L, kind):
+    """Gradients whose rows are cut into slices, shared products whose reduction is, many adapters of high rank among few rows."""
+    check(Case(N, m, n, r, L, kind, dtype))
+
+
+def test_rank_above_a_size_is_refused_on_the_device():
+    """A rank above one of the sizes (200 of a 136 x 264 projection) is no rank that the projection can have."""
+    c = Case(120, 136, 264, 200, 30, "single", BF16)
+    with pytest.raises(ab.AbError):
+        check(c)
