@@ -222,8 +222,9 @@ int ab_dense_backward(const void* x, const void* dY, const void* W, void* dX, fl
  *   has dW).  Any of dX, dA, dB may be NULL; W may be NULL where dX is.
  *   Sums are held in fp32 or more and y, dX rounded once.  Sums run in a fixed order: two runs give identical bits.  No row's result
  *   depends on another row, nor on an adapter that is not its own, also where those hold infinities or NaN; nor does dA_a or dB_a on rows
- *   that are not a's.  bf16 with m, n, r, strideA, strideB multiples of 8, r <= 256 and 16-byte aligned pointers runs on the tensor cores;
- *   everything else takes general kernels.  N = 0 is a no-op (dA, dB are zeroed).  N < 2^31.  No output may overlap an input or
+ *   that are not a's.  An infinity makes its own results infinite or NaN: the general kernels split fp32 values as ab_recombine does.
+ *   bf16 with m, n, r, strideA, strideB multiples of 8, r <= 256 and 16-byte aligned pointers runs on the tensor cores (dA and dB where
+ *   L * ceil(N / 64) <= 2^24 besides); everything else takes general kernels.  N = 0 is a no-op (dA, dB are zeroed).  N < 2^31.  No output may overlap an input or
  *   another output.  Workspace: ab_adapter_workspace_bytes, for either call.
  */
 int ab_adapter_forward(const void* x, const void* W, const void* A, const void* B, const float* scale, const int* row_adapter,
@@ -259,9 +260,10 @@ typedef struct {
  * Global norm of the gradients of a step and their scaling, between the backward calls and ab_adamw_step:
  *   norm = sqrt(sum of g^2 over all L tensors);  out = g * c,  c = max_norm / norm where norm > max_norm, else 1.
  * descs: HOST array of L descriptors (read before the call returns); tensors of type dt that start at any element; outputs overlap nothing
- * but their own gradient, if at all.  norm_out: device float.  Squares are added in 64 bits in a fixed order (no finite value
- * overflows; two runs give identical bits); out is rounded once from fp32.  A norm that is infinite or NaN scales nothing (out = g), so
- * that the caller, who finds it in norm_out, can drop the step.  max_norm >= 0; INFINITY never scales.  In place and with c = 1 nothing
+ * but their own gradient, if at all.  norm_out: device float.  Four squares at a time are added in fp32 where neither over- nor
+ * underflow is near, everything else in 64 bits, in a fixed order (no finite value overflows; two runs give identical bits); out is
+ * rounded once from fp32.  An infinity or a NaN among the gradients scales nothing (out = g), so that the caller, who finds it in
+ * norm_out, can drop the step.  (A finite norm above fp32's range reads as infinite in norm_out; the gradients are scaled.)  max_norm >= 0; INFINITY never scales.  In place and with c = 1 nothing
  * is written.  Workspace: ab_grad_clip_workspace_bytes.
  */
 int ab_grad_clip(const ab_clip_desc* descs, int L, float max_norm, float* norm_out, int dt, void* ws, size_t ws_bytes, void* cuda_stream);

@@ -349,6 +349,14 @@ def _fits(what, t, shape, dtype, dev):
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
 
+def _scratch(nbytes, device, stream):
+    """A workspace that the call owns: on a stream of the caller's it is not handed out again before that stream has run the call."""
+    ws = workspace(nbytes, device)
+    if stream is not None:
+        ws.record_stream(stream)
+    return ws
+
+
 def _adapter_ok(x, W, A, B, row_adapter, scale):
     """Checks the inputs of an adapter call; returns (N, n, L, m, r, device).  A and B may be spaced along their first axis."""
     if x.dim() != 2 or A.dim() != 3:
@@ -387,7 +395,7 @@ def ab_adapter_forward(x, W, A, B, row_adapter, scale=None, y=None, T_save=None,
     elif save_T:
         T_save = x.new_empty((N, r), dtype=torch.float32)
     if ws is None:
-        ws = workspace(ab_adapter_workspace_bytes(x, A, B), x.device)
+        ws = _scratch(ab_adapter_workspace_bytes(x, A, B), x.device, stream)
     st = lib().ab_adapter_forward(x.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), _ptr(scale), row_adapter.data_ptr(), y.data_ptr(),
                                   _ptr(T_save), N, m, n, r, L, A.stride(0), B.stride(0), _dt(x), ws.data_ptr(), ws.numel(),
                                   torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
@@ -417,7 +425,7 @@ def ab_adapter_backward(x, dY, W, A, B, row_adapter, scale=None, T_saved=None, w
     elif "dB" in want:
         dB = x.new_empty((L, r, n), dtype=torch.float32)
     if ws is None:
-        ws = workspace(ab_adapter_workspace_bytes(x, A, B), x.device)
+        ws = _scratch(ab_adapter_workspace_bytes(x, A, B), x.device, stream)
     st = lib().ab_adapter_backward(x.data_ptr(), dY.data_ptr(), _ptr(W), A.data_ptr(), B.data_ptr(), _ptr(scale), row_adapter.data_ptr(),
                                    _ptr(T_saved), _ptr(dX), _ptr(dA), _ptr(dB), N, m, n, r, L, A.stride(0), B.stride(0), _dt(x),
                                    ws.data_ptr(), ws.numel(),
@@ -471,6 +479,8 @@ class ClipPlan:
 def ab_grad_clip(plan: ClipPlan, max_norm: float, stream=None):
     """Scales the plan's gradients by max_norm / norm where their global norm is above max_norm.  Returns (outputs or None, norm), norm a
     device tensor of one fp32 value; one that is not finite scales nothing."""
+    if plan.norm.get_device() != torch.cuda.current_device():
+        raise ValueError("the plan's tensors must be on the current device")
     st = lib().ab_grad_clip(plan.descs, len(plan.grads), float(max_norm), _ptr(plan.norm), plan.dt, _ptr(plan.ws), plan.ws.numel(), _stream(stream))
     _check(st, "ab_grad_clip")
     return plan.out, plan.norm

@@ -271,7 +271,8 @@ adapter_grad_kernel(const __grid_constant__ GradSides sides, int r, const int* _
   const GradSide& w = sides.side[second];
   const TI* In = static_cast<const TI*>(w.In);
   const int P = w.P;
-  const int f0 = ((int)blockIdx.x - (second ? sides.side[0].tiles : 0)) * kGF, k0 = blockIdx.y * kGK, a = (int)blockIdx.z / slices, part = (int)blockIdx.z - a * slices;
+  const int f0 = ((int)blockIdx.x - (second ? sides.side[0].tiles : 0)) * kGF, k0 = blockIdx.y * kGK;
+  const int a = (int)blockIdx.z / slices, part = (int)blockIdx.z - a * slices;
   const int f = threadIdx.x % kGF, kq = threadIdx.x / kGF;      // this thread: column f, values 8 kq .. 8 kq + 7
   // this slice's rows, whole blocks of kGR
   const int64_t all = count[a], per = ((all + slices - 1) / slices + kGR - 1) / kGR * kGR, from = part * per < all ? part * per : all;
@@ -349,7 +350,6 @@ int base_slices(int64_t N, int P, int K) {
 // Small products stay on the fp32 pipes (128 x 512 x 256: 11.6 us against 12.0, and no slices)
 bool base_small(const Call& c, int P, int K) { return c.dt == AB_F32 && gemm_small_pays(c.N, P, K); }
 
-// Workspace of the general path: status word, T, U, the shared product, the adapters' rows
 // Slices of the rows where the gradients' tiles are few (4006 rows of one adapter, rank 4, 208 x 656: 15 blocks took 250 us)
 int grad_slices(int64_t N, int m, int n, int r, int L) {
   const int sms = sm_count() > 0 ? sm_count() : 148;
@@ -359,6 +359,7 @@ int grad_slices(int64_t N, int m, int n, int r, int L) {
   return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
 }
 
+// Workspace of the general path: status word, T, U, the shared product, the adapters' rows, the gradients' slices
 struct GeneralWs { int* status; float *T, *U, *base; int* order; int64_t *start, *count; float *pA, *pB; int slices; size_t bytes; };
 GeneralWs general_ws(void* ws, int64_t N, int m, int n, int r, int L, int dt) {
   Arena ar(ws, 0);
@@ -541,7 +542,7 @@ int ab_adapter_backward(const void* x, const void* dY, const void* W, const void
     AB_CUDA_OK(cudaMemsetAsync(ws, 0, sizeof(int), c.st));
     return AB_OK;
   }
-  if (adapter_tc_supported(c, dY, dX, T_saved, dA, dB)) {
+  if (adapter_tc_supported(c, dY, dX, T_saved, dA, dB) && ((!dA && !dB) || adapter_tc_lists_ok(N, L))) {
     if (adapter_tc_ws(N, m, n, r, L) > ws_bytes) return AB_ERR_WORKSPACE;
     return adapter_tc_backward(c, dY, T_saved, dX, dA, dB, ws);
   }

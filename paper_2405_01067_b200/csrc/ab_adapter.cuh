@@ -17,6 +17,7 @@ struct AdapterCall {
 };
 
 // sizes alone: what the workspace is for
+bool adapter_tc_lists_ok(int64_t N, int L);
 bool adapter_tc_shape_ok(int64_t N, int m, int n, int r, int L, int dt);
 bool adapter_tc_supported(const AdapterCall& c, const void* dY, const void* out, const float* T, const float* dA, const float* dB);
 size_t adapter_tc_ws(int64_t N, int m, int n, int r, int L);

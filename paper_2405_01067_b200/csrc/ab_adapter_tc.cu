@@ -240,8 +240,9 @@ __device__ __forceinline__ void rows_body(const ProjParams& p, int64_t unit, int
       if (a < 0) {
         if (part == 0) for (int k = tid; k < p.rp; k += 32 * kWarps) put_T(p, row, k, 0.f);
       } else if (!p.f_mn) {
-        // short rows leave little to load for a value: four values at a time (rank 128, rows of 160: 22 rounds of a trip to L2 each)
-        if (p.K <= 1024 && p.r >= 4 * kWarps) {
+        // short rows leave little to load for a value: four values at a time where every warp has eight or more (rank 128, rows of 160: 22
+        // rounds of a trip to L2 each; rank 24, rows of 776: 24.7 us one at a time, 25.9 in fours)
+        if (p.K <= 1024 && p.r >= 8 * kWarps) {
           for (int k = (part * kWarps + warp) * 4; k < p.rp; k += parts * kWarps * 4) {
             const uint4* f[4];
             float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -1488,7 +1489,8 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   p.f_bytes = f_mn ? (cols + 63) / 64 * 8192 : cols * 128;
   p.csize = 8;
   while (p.csize > 1 && (tiles * p.csize > 2 * sms || 2 * p.csize > p.nk)) p.csize >>= 1;
-  // Up to three CTAs an SM, and no more room than for as many as there are: CTAs fill an SM before they go to the next.  The ring takes the
+  // Never more CTAs an SM than TMEM has columns for (three of 128, two of 256): one that waited for columns would hold up its cluster, whose
+  // others hold theirs.  Up to three CTAs an SM, and no more room than for as many as there are: CTAs fill an SM before they go to the next.  The ring takes the
   // parts at the end.
   const int64_t each = (tiles * p.csize * ((rp + 127) / 128) + (c.N <= 2048 ? units : 0) + sms - 1) / sms;
   // room for the factors of two adapters at once where that leaves as many CTAs their place
@@ -1497,7 +1499,7 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   if (p.q_max > kMaxAd) p.q_max = kMaxAd;
   p.slot_bytes = p.in_bytes + room;
   if (p.slot_bytes < 16384) p.slot_bytes = 16384;          // an MMA reads 128 rows of In, loaded or not
-  const int parts = p.tile_rows * (cols + 4) * 4, budget = each <= 1 ? 120 * 1024 : each == 2 ? 96 * 1024 : 72 * 1024;
+  const int parts = p.tile_rows * (cols + 4) * 4, budget = each <= 1 ? 120 * 1024 : each == 2 || cols > 64 ? 96 * 1024 : 72 * 1024;
   p.ns = budget / p.slot_bytes < 3 ? 3 : budget / p.slot_bytes < kMaxStages ? budget / p.slot_bytes : kMaxStages;
   if (p.ns * p.slot_bytes < parts) p.ns = (parts + p.slot_bytes - 1) / p.slot_bytes;
   p.tmem_cols = 2 * pow2_cols(p.q_max * cols);
@@ -1619,7 +1621,7 @@ TcWs tc_ws(void* ws, int64_t N, int m, int n, int r, int L) {
   w.TP = ar.take_n<bf16>((size_t)N * 3 * rp);
   w.UP = ar.take_n<bf16>((size_t)N * 3 * rp);
   w.nslab = (int)((N + 63) / 64);
-  w.list = ar.take_n<uint4>((size_t)L * w.nslab);
+  w.list = adapter_tc_lists_ok(N, L) ? ar.take_n<uint4>((size_t)L * w.nslab) : nullptr;
   w.count = ar.take_n<int>((size_t)L);
   w.slices = grad_slices(N, m, n, r, L);
   w.pA = w.slices > 1 ? ar.take_n<float>((size_t)w.slices * L * m * r) : nullptr;
@@ -1678,6 +1680,9 @@ int launch_grads(const AdapterCall& c, const void* dY, float* dA, float* dB, con
 }
 
 }  // namespace
+
+// The gradients' slab lists take 16 bytes an adapter and 64 rows: up to 256 MB.
+bool adapter_tc_lists_ok(int64_t N, int L) { return (N + 63) / 64 * L <= ((int64_t)1 << 24); }
 
 bool adapter_tc_shape_ok(int64_t N, int m, int n, int r, int L, int dt) {
   return dt == AB_BF16 && m % 8 == 0 && n % 8 == 0 && r % 8 == 0 && r <= 256 && N <= ((int64_t)1 << 30) && L < (1 << 30);

@@ -79,3 +79,8 @@ def test_clip_refusals(b):
     assert clip(b, [(4096, 4096, 3), (8192, None, 3)]) == bad          # all are scaled or none is
     assert clip(b, [(4096, 4096, (1 << 40) + 1)]) == b.AB_ERR_UNSUPPORTED
     assert b.lib().ab_grad_clip_workspace_bytes(0) == 0 and b.lib().ab_grad_clip_workspace_bytes(5) >= 256
+
+
+def test_workspace_of_many_adapters_stays_small(b):
+    """The lists behind the gradients are bounded whatever the number of adapters: 2^20 adapters beside 2^20 rows."""
+    assert 0 < b.lib().ab_adapter_workspace_bytes(1 << 20, 64, 64, 8, 1 << 20, b.AB_BF16) < 1 << 31

@@ -3,8 +3,6 @@
 Tolerances, element by element.  With S the same sum over absolute values, K terms of fp32 lose at most K 2^-23 S (also where a sum is
 cut off instead of rounded at every step); T and U are carried on with 16 bits at least (2^-16 of the second product's S); a result
 held in bf16 is off by half a step of itself, 2^-8."""
-import ctypes
-
 import numpy as np
 import pytest
 import torch
@@ -414,3 +412,44 @@ def test_rank_above_a_size_is_refused_on_the_device():
     c = Case(120, 136, 264, 200, 30, "single", BF16)
     with pytest.raises(ab.AbError):
         check(c)
+
+
+def test_more_adapters_than_lists_hold():
+    """Beyond 2^24 entries of the slab lists the gradients go by the general kernels, whose results are the same sums."""
+    N, L, m, n, r = 64 * 900 - 5, 20000, 16, 24, 8
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, dY = (torch.randn(N, k, device="cuda", generator=g).bfloat16() for k in (n, m))
+    W = (torch.randn(m, n, device="cuda", generator=g) / n ** 0.5).bfloat16()
+    A = torch.randn(L, m, r, device="cuda", generator=g).bfloat16()
+    B = torch.randn(L, r, n, device="cuda", generator=g).bfloat16()
+    ids = torch.randint(-1, L, (N,), device="cuda", generator=g, dtype=torch.int32)
+    y, T = ab.ab_adapter_forward(x, W, A, B, ids, save_T=True)
+    dX, dA, dB = ab.ab_adapter_backward(x, dY, W, A, B, ids, T_saved=T)
+    has, a = (ids >= 0).double()[:, None], ids.clamp(min=0).long()
+    xd, yd, Ad, Bd = x.double(), dY.double(), A.double()[a], B.double()[a]
+    t = has * torch.einsum("irn,in->ir", Bd, xd)
+    u = has * torch.einsum("imr,im->ir", Ad, yd)
+    want_y = xd @ W.double().T + torch.einsum("imr,ir->im", Ad, t)
+    want_dX = yd @ W.double() + torch.einsum("irn,ir->in", Bd, u)
+    want_dA = torch.zeros(L, m, r, device="cuda", dtype=torch.float64).index_add_(0, a, yd[:, :, None] * t[:, None, :])
+    want_dB = torch.zeros(L, r, n, device="cuda", dtype=torch.float64).index_add_(0, a, u[:, :, None] * xd[:, None, :])
+    # y, dX: half a step of bf16; dA, dB: sums of up to 24 products of 8 to 24 terms in fp32 (24 + 24 roundings of 2^-24)
+    for got, want, tol in ((y, want_y, 2.0 ** -8), (dX, want_dX, 2.0 ** -8), (dA, want_dA, 48 * 2.0 ** -24), (dB, want_dB, 48 * 2.0 ** -24)):
+        assert float((got.double() - want).norm() / want.norm()) < tol
+
+
+def test_a_stream_of_the_caller_keeps_its_workspace():
+    """A workspace that the call allocates is not handed out again while a side stream still uses it."""
+    c = Case(700, 264, 512, 24, 5, "mixed", BF16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    x, _, W, A, B, ids, scale = c.cuda()
+    want, _ = ab.ab_adapter_forward(x, W, A, B, ids, scale)
+    torch.cuda.synchronize()
+    y = torch.empty_like(want)
+    for _ in range(20):
+        ab.ab_adapter_forward(x, W, A, B, ids, scale, y=y, stream=side)
+        junk = [torch.full((1 << 16,), 255, dtype=torch.uint8, device="cuda") for _ in range(40)]
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+        del junk
