@@ -16,7 +16,7 @@
 //
 // Measured, us (floor: the bytes or operations a call cannot do without, at 6538 GB/s and 1679 TFLOP/s): one token, 4096 x 4096, rank 16 16
 // (5.2); 64 tokens of 64 adapters 17 (7.9); 6173 rows of 16 adapters, 2048 -> 8192, rank 64 214 (128; wide_kernel 1180 TFLOP/s);
-// training, 50,432 rows of 4 groups, 768 x 768, rank 64 242 (89); 8191 rows of 8, 4096 x 4096, rank 16 505 (331).
+// training, 50,432 rows of 4 groups, 768 x 768, rank 64 237 (89); 8191 rows of 8, 4096 x 4096, rank 16 505 (331).
 //
 // T travels as three bf16 pieces (hi = bf16(T), mid = bf16(T - hi), lo the rest: 24 bits): the second product takes two of them (its result
 // is rounded to bf16, 2^-17 of T is lost), the gradients take all three.
@@ -101,8 +101,9 @@ __device__ __forceinline__ void raise(int* abort_any, int* status) {
 
 // ------------------------------------------------------------------------------------------------ what a backward call prepares
 // CTAs 0 .. L-1: the 64-row slabs that have rows of adapter `cta`, ascending: (slab, which of its rows are the adapter's: 32 bits and 32 bits,
-// 0).  CTAs behind: T (fp32) cut into pieces, eight values a thread.  Reads the call's inputs alone: it runs beside the projection, in
-// one launch with it (a launch of its own found no room before the kernel in front of it had ended: 20 us for the ViT groups).
+// 0).  CTAs behind: T (fp32) cut into pieces, eight values a thread.  Reads the call's inputs alone: the lists are made beside the
+// projection, in one launch with it, and its tiles' CTAs cut T (a launch of its own found no room before the kernel in front of it had
+// ended: 20 us for the ViT groups).
 struct PrepParams {
   uint4* list; int* count; int nslab;
   const float* T; bf16* P;
@@ -210,7 +211,8 @@ struct ProjParams {
   int* status;
   // project_tc_kernel
   int prep_ctas, tile_ctas;                 // CTAs that prepare, whole clusters (they come first: lists are chains), and that have tiles
-  PrepParams prep;
+  PrepParams prep;                          // ctas: lists alone; T is cut by the CTAs that have the tiles (cut)
+  int cut;
   int nk, csize, ns, slot_bytes, in_bytes, f_bytes, q_max, tmem_cols;
 };
 
@@ -503,6 +505,33 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmIn, const __grid_constan
       const unsigned same = __ballot_sync(0xffffffffu, a == g0 || !live);
       const bool mixed = ((same >> (lane & 16)) & 0xffffu) != 0xffffu;
       b->row_ad[lrow] = !live || (mixed && !b->whole) ? -2 : p.want_T ? (a < 0 ? 0x7fffffff : a | 0x40000000) : a;
+    }
+    // These warps have nothing to do before the first slabs have been multiplied: they cut this CTA's share of the saved T.  (By CTAs of their
+    // own in front of the tiles the ViT groups took 241 us, behind them 245, here 237.)
+    if (p.cut && blockIdx.y == 0) {
+      const int part = p.tile_rows / p.csize, oct = p.rp / 8;
+      const int64_t r0 = row0 + rank * part;
+      const int n = r0 >= p.N ? 0 : (int)(p.N - r0 < part ? p.N - r0 : part) * oct;
+      for (int i0 = threadIdx.x - 64; i0 < n; i0 += 4 * 128) {
+        float4 t[4][2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = i0 + e * 128, lr = i / oct, k = (i - lr * oct) * 8;
+          t[e][0] = t[e][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (i < n && k < p.r) {
+            const float4* q = reinterpret_cast<const float4*>(p.prep.T + (r0 + lr) * p.r + k);
+            t[e][0] = q[0];
+            t[e][1] = q[1];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = i0 + e * 128, lr = i / oct, k = (i - lr * oct) * 8;
+          if (i >= n) break;
+          const float v[8] = {t[e][0].x, t[e][0].y, t[e][0].z, t[e][0].w, t[e][1].x, t[e][1].y, t[e][1].z, t[e][1].w};
+          put_pieces(p.prep.P + (r0 + lr) * 3 * p.rp + k, p.rp, v);
+        }
+      }
     }
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
@@ -1512,8 +1541,10 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   AB_TRY(make_tensor_map_2d(&tmIn, In, false, (uint64_t)c.N, K, K, 64, p.tile_rows));
   AB_TRY(stack_map(&tmF, c, F, f_mn ? K : c.r, f_mn ? c.r : K, strideF, f_mn ? 64 : cols));
   p.tile_ctas = (int)(tiles * p.csize);
-  if (prep) {                               // taken along
+  if (prep && prep->ctas > 0) {             // taken along
     p.prep = *prep;
+    p.cut = prep->ctas > c.L ? 1 : 0;
+    p.prep.ctas = c.L;
     prep->ctas = 0;
   }
   p.prep_ctas = (p.prep.ctas + p.csize - 1) / p.csize * p.csize;
