@@ -317,16 +317,26 @@ adapter_grad_kernel(const __grid_constant__ GradSides sides, int r, const int* _
     if (k0 + 8 * kq + e < r) d[(k0 + 8 * kq + e) * w.d_k] = (float)acc[e];
 }
 
-// out[i] = sum over the slices, in their order
+// out[i] = sum over the slices, in their order, for one or two results in one launch
+struct SliceSide { const float* part; float* out; int64_t count; };
 __global__ void __launch_bounds__(256)
-add_slices_kernel(const float* __restrict__ part, float* __restrict__ out, int64_t count, int slices) {
+add_slices_kernel(SliceSide x, SliceSide y, int slices) {
   tc::dep_wait();
   tc::dep_launch();
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= count) return;
-  float v = part[i];
-  for (int s = 1; s < slices; ++s) v += part[s * count + i];
-  out[i] = v;
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const bool second = i >= x.count;
+  if (second) i -= x.count;
+  const SliceSide& w = second ? y : x;
+  if (i >= w.count) return;
+  float v = 0.f;
+  for (int s0 = 0; s0 < slices; s0 += 8) {
+    float u[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) u[s] = s0 + s < slices ? __ldcg(w.part + (s0 + s) * w.count + i) : 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) v += u[s];
+  }
+  w.out[i] = v;
 }
 
 typedef AdapterCall Call;
@@ -456,9 +466,7 @@ int grads(const Call& c, const GeneralWs& w, const void* dY, const float* T, flo
     for (int i = 0; i < n; ++i) s.side[i].D += step * s.side[i].strideD;
   }
   if (w.slices == 1) return AB_OK;
-  if (dA) AB_TRY(launch_after(add_slices_kernel, (unsigned)((ea + 255) / 256), 256u, 0, 1, c.st, (const float*)w.pA, dA, ea, w.slices));
-  if (dB) AB_TRY(launch_after(add_slices_kernel, (unsigned)((eb + 255) / 256), 256u, 0, 1, c.st, (const float*)w.pB, dB, eb, w.slices));
-  return AB_OK;
+  return adapter_add_slices(w.pA, dA, ea, w.pB, dB, eb, w.slices, c.st);
 }
 
 int general_forward(const Call& c, void* y, float* T_save, const GeneralWs& w) {
@@ -491,6 +499,12 @@ int check_args(const Call& c) {
 }
 
 }  // namespace
+
+int adapter_add_slices(const float* pA, float* dA, int64_t ea, const float* pB, float* dB, int64_t eb, int slices, cudaStream_t st) {
+  const SliceSide x{pA, dA, dA ? ea : 0}, y{pB, dB, dB ? eb : 0};
+  return launch_after(add_slices_kernel, (unsigned)((x.count + y.count + 255) / 256), 256u, 0, 1, st, x, y, slices);
+}
+
 }  // namespace ab
 
 using namespace ab;

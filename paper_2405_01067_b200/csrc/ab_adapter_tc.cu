@@ -1707,11 +1707,8 @@ int launch_grads(const AdapterCall& c, const void* dY, float* dA, float* dB, con
     AB_CUDA_OK(allow_smem(adapter_grad_tc_kernel<8>));
     AB_TRY(launch_after(adapter_grad_tc_kernel<8>, (unsigned)grid, (unsigned)kWideThreads, smem, 1, c.st, act[0], small[0], act[1], small[1], p));
   }
-  if (w.slices > 1) {
-    const int64_t ea = (int64_t)c.L * c.m * c.r, eb = (int64_t)c.L * c.n * c.r;
-    if (dA) AB_TRY(sum_slices(w.pA, dA, ea, ea, w.slices, c.st));
-    if (dB) AB_TRY(sum_slices(w.pB, dB, eb, eb, w.slices, c.st));
-  }
+  if (w.slices > 1)
+    return adapter_add_slices(w.pA, dA, (int64_t)c.L * c.m * c.r, w.pB, dB, (int64_t)c.L * c.n * c.r, w.slices, c.st);
   return AB_OK;
 }
 
