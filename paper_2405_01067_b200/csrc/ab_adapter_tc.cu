@@ -661,30 +661,38 @@ __device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t (&a)[4
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
+// A lane's words of G_a for 32 features and 64 values of r: as mma.sync wants them where a feature's values lie together, else (p.mn) by
+// 8 x 8 blocks as they lie, a row of r a lane group, to be transposed by turn_g (two 2-byte loads for each word instead: 5625 rows, 72 -> 536,
+// rank 72, five adapters in any order, took 207 us in this kernel).
 __device__ __forceinline__ void load_g(const OutParams& p, int a, int f0, int k0, int kn, int lane, uint32_t (&u)[2][4][4]) {
   const bf16* g = p.G + a * p.strideG;
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {            // a feature past the last one reads what the last one does
+    for (int x = 0; x < 2; ++x) {            // a feature past the last one reads what the last ones do (P is a multiple of 8)
       const int f = f0 + 16 * h + 8 * x + (lane >> 2), ff = f < p.P ? f : p.P - 1;
+      const int b0 = f0 + 16 * h + 8 * x, fb = b0 < p.P ? b0 : p.P - 8;
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          const int k = k0 + 16 * kk + 8 * y + 2 * (lane & 3);
+          const int k = k0 + 16 * kk + 8 * y;
           uint32_t w = 0u;
           if (16 * kk + 8 * y < kn) {
-            if (!p.mn) {
-              w = *reinterpret_cast<const uint32_t*>(g + (int64_t)ff * p.r + k);
-            } else {
-              const unsigned short* q = reinterpret_cast<const unsigned short*>(g) + (int64_t)k * p.P + ff;
-              w = (uint32_t)q[0] | ((uint32_t)q[p.P] << 16);
-            }
+            if (!p.mn) w = *reinterpret_cast<const uint32_t*>(g + (int64_t)ff * p.r + k + 2 * (lane & 3));
+            else w = *reinterpret_cast<const uint32_t*>(g + (int64_t)(k + (lane >> 2)) * p.P + fb + 2 * (lane & 3));
           }
           u[h][kk][2 * y + x] = w;
         }
     }
+}
+__device__ __forceinline__ void turn_g(uint32_t (&u)[2][4][4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(u[h][kk][i]));
 }
 __device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int id, int f0, int lane, uint32_t (&v)[2][16]) {
   const unsigned live = __ballot_sync(0xffffffffu, id >= 0);
@@ -715,6 +723,7 @@ __device__ __forceinline__ void add_mixed(const OutParams& p, int64_t row0, int 
 #pragma unroll 1
     while (true) {
       const unsigned rows = __shfl_sync(0xffffffffu, same, h) & live;
+      if (p.mn) turn_g(g);
       float c[2][4][4];
 #pragma unroll
       for (int m = 0; m < 2; ++m)
