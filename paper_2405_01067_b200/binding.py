@@ -402,13 +402,13 @@ def ab_adapter_forward(x, W, A, B, row_adapter, scale=None, y=None, T_save=None,
         raise ValueError("the shared projection W is wanted in a forward call")
     N, n, L, m, r, dev = _adapter_ok(x, W, A, B, row_adapter, scale)
     if y is None:
-        y = x.new_empty((N, m))
+        y = x.new_empty((N, m)) if stream is None else _result(x, (N, m), stream)
     else:
         _fits("y", y, (N, m), x.dtype, dev)
     if T_save is not None:
         _fits("T_save", T_save, (N, r), torch.float32, dev)
     elif save_T:
-        T_save = x.new_empty((N, r), dtype=torch.float32)
+        T_save = _result(x, (N, r), stream, torch.float32)
     if ws is None:
         ws = _scratch(ab_adapter_workspace_bytes(x, A, B), x.device, stream)
     st = lib().ab_adapter_forward(x.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), _ptr(scale), row_adapter.data_ptr(), y.data_ptr(),
@@ -430,15 +430,15 @@ def ab_adapter_backward(x, dY, W, A, B, row_adapter, scale=None, T_saved=None, w
     if dX is not None:
         _fits("dX", dX, (N, n), x.dtype, dev)
     elif "dX" in want:
-        dX = x.new_empty((N, n))
+        dX = x.new_empty((N, n)) if stream is None else _result(x, (N, n), stream)
     if dA is not None:
         _fits("dA", dA, (L, m, r), torch.float32, dev)
     elif "dA" in want:
-        dA = x.new_empty((L, m, r), dtype=torch.float32)
+        dA = _result(x, (L, m, r), stream, torch.float32)
     if dB is not None:
         _fits("dB", dB, (L, r, n), torch.float32, dev)
     elif "dB" in want:
-        dB = x.new_empty((L, r, n), dtype=torch.float32)
+        dB = _result(x, (L, r, n), stream, torch.float32)
     if ws is None:
         ws = _scratch(ab_adapter_workspace_bytes(x, A, B), x.device, stream)
     st = lib().ab_adapter_backward(x.data_ptr(), dY.data_ptr(), _ptr(W), A.data_ptr(), B.data_ptr(), _ptr(scale), row_adapter.data_ptr(),

@@ -47,7 +47,22 @@ def clip(norm_only=False):
     return call
 
 
-CALLS = {"clip": clip, "clip_norm": lambda: clip(True)}
+def adapters(back, dtype, N, m, n):
+    x, dY, W = normal(N, n, seed=1, dtype=dtype), normal(N, m, seed=2, dtype=dtype), normal(m, n, seed=3, dtype=dtype)
+    A, B = normal(3, m, 16, seed=4, dtype=dtype), normal(3, 16, n, seed=5, dtype=dtype)
+    ids = (torch.arange(N, device="cuda", dtype=torch.int32) * 7 // N) % 4 - 1
+
+    def call(stream=None):
+        if back:
+            return ab.ab_adapter_backward(x, dY, W, A, B, ids, stream=stream)
+        return ab.ab_adapter_forward(x, W, A, B, ids, stream=stream, save_T=True)
+    call.made = 3 if back else 2
+    return call
+
+
+CALLS = {"clip": clip, "clip_norm": lambda: clip(True),
+         "adapter_forward": lambda: adapters(False, BF16, 1500, 264, 200), "adapter_backward": lambda: adapters(True, BF16, 1500, 264, 200),
+         "adapter_forward_few": lambda: adapters(False, BF16, 5, 72, 88), "adapter_backward_fp32": lambda: adapters(True, F32, 300, 101, 77)}
 
 
 @pytest.fixture(autouse=True)
