@@ -210,14 +210,14 @@ def _scratch(nbytes, device, stream):
         return workspace(nbytes, device)
 
 
-def _result(x, shape, stream, dtype=None):
+def _result(x, shape, stream, dtype=None, zero=False):
     """A tensor on x's device (of x's type, unless given) that a call returns: the caller reads it on the current stream, behind a wait
     of theirs, and its memory is kept until that has run too."""
     if stream is None:
-        return x.new_empty(shape, dtype=dtype)
+        return x.new_zeros(shape, dtype=dtype) if zero else x.new_empty(shape, dtype=dtype)
     here = torch.cuda.current_stream(x.device)
     with torch.cuda.stream(stream):
-        t = x.new_empty(shape, dtype=dtype)
+        t = x.new_zeros(shape, dtype=dtype) if zero else x.new_empty(shape, dtype=dtype)
     t.record_stream(here)
     return t
 
@@ -238,11 +238,11 @@ def ab_layer_forward(x, A, B, y=None, T_save=None, ws=None, stream=None, save_T=
     m, r = A.shape
     dt = _dt(x)
     if y is None:
-        y = torch.empty((N, m), dtype=x.dtype, device=x.device)
+        y = _result(x, (N, m), stream)
     if save_T and T_save is None:
-        T_save = torch.empty((N, r), dtype=x.dtype, device=x.device)
+        T_save = _result(x, (N, r), stream)
     if ws is None:
-        ws = workspace(ab_workspace_bytes(AB_OP_LAYER_FORWARD, N, m, n, r, 1, dt), x.device)
+        ws = _scratch(ab_workspace_bytes(AB_OP_LAYER_FORWARD, N, m, n, r, 1, dt), x.device, stream)
     st = lib().ab_layer_forward(_ptr(x), _ptr(A), _ptr(B), _ptr(y), _ptr(T_save), N, m, n, r,
                                 A.stride(0), B.stride(0), dt, _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "ab_layer_forward")
@@ -270,13 +270,13 @@ def ab_layer_backward(x, dY, A, B, T_saved=None, want=("dX", "dA", "dB"), dX=Non
     m, r = A.shape
     dt = _dt(x)
     if "dX" in want and dX is None:
-        dX = torch.empty((N, n), dtype=x.dtype, device=x.device)
+        dX = _result(x, (N, n), stream)
     if "dA" in want and dA is None:
-        dA = torch.empty((m, r), dtype=torch.float32, device=x.device)
+        dA = _result(x, (m, r), stream, torch.float32)
     if "dB" in want and dB is None:
-        dB = torch.empty((r, n), dtype=torch.float32, device=x.device)
+        dB = _result(x, (r, n), stream, torch.float32)
     if ws is None:
-        ws = workspace(ab_workspace_bytes(AB_OP_LAYER_BACKWARD, N, m, n, r, 1, dt), x.device)
+        ws = _scratch(ab_workspace_bytes(AB_OP_LAYER_BACKWARD, N, m, n, r, 1, dt), x.device, stream)
     st = lib().ab_layer_backward(_ptr(x), _ptr(dY), _ptr(A), _ptr(B), _ptr(T_saved), _ptr(dX), _ptr(dA), _ptr(dB),
                                  N, m, n, r, A.stride(0), B.stride(0), dt, _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "ab_layer_backward")
@@ -293,11 +293,11 @@ def ab_conv3x3_forward(x, A, B, y=None, T_save=None, ws=None, stream=None, save_
     batch, H, W, C = x.shape
     m, r = A.shape
     if y is None:
-        y = torch.empty((batch, H, W, m), dtype=x.dtype, device=x.device)
+        y = _result(x, (batch, H, W, m), stream)
     if save_T and T_save is None:
-        T_save = torch.empty((batch * H * W, r), dtype=x.dtype, device=x.device)
+        T_save = _result(x, (batch * H * W, r), stream)
     if ws is None:
-        ws = workspace(ab_conv3x3_workspace_bytes(batch, H, W, C, m, r), x.device)
+        ws = _scratch(ab_conv3x3_workspace_bytes(batch, H, W, C, m, r), x.device, stream)
     st = lib().ab_conv3x3_forward(_ptr(x), _ptr(A), _ptr(B), _ptr(y), _ptr(T_save), batch, H, W, C, m, r,
                                   A.stride(0), B.stride(0), _dt(x), _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "ab_conv3x3_forward")
@@ -311,13 +311,13 @@ def ab_conv3x3_backward(x, dY, A, B, T_saved=None, want=("dX", "dA", "dB"), dX=N
     batch, H, W, C = x.shape
     m, r = A.shape
     if "dX" in want and dX is None:
-        dX = torch.empty_like(x)
+        dX = _result(x, x.shape, stream)
     if "dA" in want and dA is None:
-        dA = torch.empty((m, r), dtype=torch.float32, device=x.device)
+        dA = _result(x, (m, r), stream, torch.float32)
     if "dB" in want and dB is None:
-        dB = torch.empty((r, 9 * C), dtype=torch.float32, device=x.device)
+        dB = _result(x, (r, 9 * C), stream, torch.float32)
     if ws is None:
-        ws = workspace(ab_conv3x3_workspace_bytes(batch, H, W, C, m, r), x.device)
+        ws = _scratch(ab_conv3x3_workspace_bytes(batch, H, W, C, m, r), x.device, stream)
     st = lib().ab_conv3x3_backward(_ptr(x), _ptr(dY), _ptr(A), _ptr(B), _ptr(T_saved), _ptr(dX), _ptr(dA), _ptr(dB),
                                    batch, H, W, C, m, r, A.stride(0), B.stride(0), _dt(x), _ptr(ws), ws.numel(),
                                    _stream(stream))
@@ -332,9 +332,9 @@ def ab_dense_forward(x, W, y=None, ws=None, stream=None):
     m = W.shape[0]
     dt = _dt(x)
     if y is None:
-        y = torch.empty((N, m), dtype=x.dtype, device=x.device)
+        y = _result(x, (N, m), stream)
     if ws is None:
-        ws = workspace(ab_workspace_bytes(AB_OP_DENSE_FORWARD, N, m, n, 0, 1, dt), x.device)
+        ws = _scratch(ab_workspace_bytes(AB_OP_DENSE_FORWARD, N, m, n, 0, 1, dt), x.device, stream)
     st = lib().ab_dense_forward(_ptr(x), _ptr(W), _ptr(y), N, m, n, dt, _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "ab_dense_forward")
     return y
@@ -347,11 +347,11 @@ def ab_dense_backward(x, dY, W, want=("dX", "dW"), dX=None, dW=None, ws=None, st
     m = W.shape[0]
     dt = _dt(x)
     if "dX" in want and dX is None:
-        dX = torch.empty((N, n), dtype=x.dtype, device=x.device)
+        dX = _result(x, (N, n), stream)
     if "dW" in want and dW is None:
-        dW = torch.empty((m, n), dtype=torch.float32, device=x.device)
+        dW = _result(x, (m, n), stream, torch.float32)
     if ws is None:
-        ws = workspace(ab_workspace_bytes(AB_OP_DENSE_BACKWARD, N, m, n, 0, 1, dt), x.device)
+        ws = _scratch(ab_workspace_bytes(AB_OP_DENSE_BACKWARD, N, m, n, 0, 1, dt), x.device, stream)
     st = lib().ab_dense_backward(_ptr(x), _ptr(dY), _ptr(W), _ptr(dX), _ptr(dW), N, m, n, dt, _ptr(ws), ws.numel(),
                                  _stream(stream))
     _check(st, "ab_dense_backward")
@@ -531,7 +531,7 @@ def ab_group_average(copies, out=None, out_dtype=None, stream=None):
     K = copies.shape[0]
     count = copies[0].numel()
     if out is None:
-        out = torch.empty(copies.shape[1:], dtype=out_dtype or torch.float32, device=copies.device)
+        out = _result(copies, copies.shape[1:], stream, out_dtype or torch.float32)
     st = lib().ab_group_average(_ptr(copies), copies.stride(0) if K > 1 else count, K, count, _dt(copies), _dt(out),
                                 _ptr(out), _stream(stream))
     _check(st, "ab_group_average")
@@ -544,9 +544,9 @@ def ab_recombine(Abar, Bbar, W=None, ws=None, stream=None):
     m, r = Abar.shape
     n = Bbar.shape[1]
     if W is None:
-        W = torch.empty((m, n), dtype=torch.float32, device=Abar.device)
+        W = _result(Abar, (m, n), stream, torch.float32)
     if ws is None:
-        ws = workspace(ab_workspace_bytes(AB_OP_RECOMBINE, 0, m, n, r, 1, _dt(Abar)), Abar.device)
+        ws = _scratch(ab_workspace_bytes(AB_OP_RECOMBINE, 0, m, n, r, 1, _dt(Abar)), Abar.device, stream)
     st = lib().ab_recombine(_ptr(Abar), _ptr(Bbar), _ptr(W), m, n, r, Abar.stride(0), Bbar.stride(0), _dt(Abar),
                             _ptr(ws), ws.numel(), _stream(stream))
     _check(st, "ab_recombine")
@@ -559,13 +559,12 @@ def ab_recombine_mean(A_copies, B_copies, W=None, Abar=None, Bbar=None, want_mea
     _dev_ok(A_copies, B_copies, W, Abar, Bbar)
     K, m, r = A_copies.shape
     n = B_copies.shape[2]
-    dev = A_copies.device
     if W is None:
-        W = torch.empty((m, n), dtype=torch.float32, device=dev)
+        W = _result(A_copies, (m, n), stream, torch.float32)
     if want_means and Abar is None:
-        Abar = torch.empty((m, r), dtype=torch.float32, device=dev)
+        Abar = _result(A_copies, (m, r), stream, torch.float32)
     if want_means and Bbar is None:
-        Bbar = torch.empty((r, n), dtype=torch.float32, device=dev)
+        Bbar = _result(A_copies, (r, n), stream, torch.float32)
     st = lib().ab_recombine_mean(_ptr(A_copies), A_copies.stride(0) if K > 1 else m * r, _ptr(B_copies),
                                  B_copies.stride(0) if K > 1 else r * n, K, _ptr(W), _ptr(Abar), _ptr(Bbar), m, n, r,
                                  _dt(A_copies), _stream(stream))
@@ -580,13 +579,13 @@ def ab_svd_split(W, r_max, sigma_cutoff=0.0, out_dtype=None, ws=None, stream=Non
     m, n = W.shape
     od = out_dtype or W.dtype
     r_cap = min(r_max, m, n)
-    A = torch.empty((m, r_max), dtype=od, device=W.device)
-    B = torch.empty((r_max, n), dtype=od, device=W.device)
-    sigma = torch.empty((r_cap,), dtype=torch.float32, device=W.device)
-    r_out = torch.zeros((1,), dtype=torch.int32, device=W.device)
-    status = torch.zeros((1,), dtype=torch.int32, device=W.device)
+    A = _result(W, (m, r_max), stream, od)
+    B = _result(W, (r_max, n), stream, od)
+    sigma = _result(W, (r_cap,), stream, torch.float32)
+    r_out = _result(W, (1,), stream, torch.int32, zero=True)
+    status = _result(W, (1,), stream, torch.int32, zero=True)
     if ws is None:
-        ws = workspace(ab_workspace_bytes(AB_OP_SVD_SPLIT, 0, m, n, r_max, 1, _dt(W)), W.device)
+        ws = _scratch(ab_workspace_bytes(AB_OP_SVD_SPLIT, 0, m, n, r_max, 1, _dt(W)), W.device, stream)
     st = lib().ab_svd_split(_ptr(W), m, n, r_max, float(sigma_cutoff), _ptr(A), _ptr(B), _ptr(sigma), _ptr(r_out),
                             _ptr(status), _dt(W), AB_BF16 if od == torch.bfloat16 else AB_F32, _ptr(ws), ws.numel(),
                             _stream(stream))
@@ -595,7 +594,8 @@ def ab_svd_split(W, r_max, sigma_cutoff=0.0, out_dtype=None, ws=None, stream=Non
 
 
 class SyncPlan:
-    """Buffers and descriptors of one model's group synchronisation (ab_group_sync)."""
+    """Buffers and descriptors of one model's group synchronisation (ab_group_sync).  The buffers belong to the stream that the plan is made
+    on: another one that runs the call waits for that first, and the plan stays until it has run it."""
 
     def __init__(self, A_copies, B_copies, sigma_cutoff, want_W=False, strided=False):
         """A_copies[i]: (K, m, r), B_copies[i]: (K, r, n).  strided=True accepts views whose copies are

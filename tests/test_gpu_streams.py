@@ -60,8 +60,53 @@ def adapters(back, dtype, N, m, n):
     return call
 
 
+def layer(back, dtype):
+    x, dY, A, B = (normal(*s, seed=k, dtype=dtype) for k, s in enumerate([(1000, 200), (1000, 264), (264, 16), (16, 200)]))
+
+    def call(stream=None):
+        if back:
+            return ab.ab_layer_backward(x, dY, A, B, stream=stream)
+        return ab.ab_layer_forward(x, A, B, stream=stream, save_T=True)
+    call.made = 3 if back else 2
+    return call
+
+
+def conv(back):
+    x, dY, A, B = (normal(*s, seed=k, dtype=BF16) for k, s in enumerate([(3, 9, 10, 16), (3, 9, 10, 24), (24, 16), (16, 144)]))
+
+    def call(stream=None):
+        if back:
+            return ab.ab_conv3x3_backward(x, dY, A, B, stream=stream)
+        return ab.ab_conv3x3_forward(x, A, B, stream=stream, save_T=True)
+    call.made = 3 if back else 2
+    return call
+
+
+def dense(back, dtype):
+    x, dY, W = (normal(*s, seed=k, dtype=dtype) for k, s in enumerate([(900, 200), (900, 264), (264, 200)]))
+
+    def call(stream=None):
+        return ab.ab_dense_backward(x, dY, W, stream=stream) if back else ab.ab_dense_forward(x, W, stream=stream)
+    call.made = 2 if back else 1
+    return call
+
+
+def sync(which):
+    A, B = normal(3, 200, 16), normal(3, 16, 264, seed=1)
+    W = (A[0] @ B[0]).contiguous()
+    call = {"average": lambda stream=None: ab.ab_group_average(A, stream=stream), "recombine": lambda stream=None: ab.ab_recombine(A[0], B[0], stream=stream),
+            "mean": lambda stream=None: ab.ab_recombine_mean(A, B, stream=stream), "split": lambda stream=None: ab.ab_svd_split(W, 16, 0.05, stream=stream)}[which]
+    call.made = {"average": 1, "recombine": 1, "mean": 3, "split": 5}[which]
+    call.scratch = which in ("recombine", "split")
+    return call
+
+
 CALLS = {"clip": clip, "clip_norm": lambda: clip(True),
          "adapter_forward": lambda: adapters(False, BF16, 1500, 264, 200), "adapter_backward": lambda: adapters(True, BF16, 1500, 264, 200),
+         "layer_forward": lambda: layer(False, BF16), "layer_backward": lambda: layer(True, BF16), "layer_backward_fp32": lambda: layer(True, F32),
+         "conv_forward": lambda: conv(False), "conv_backward": lambda: conv(True), "dense_forward": lambda: dense(False, BF16),
+         "dense_backward": lambda: dense(True, BF16), "dense_backward_fp32": lambda: dense(True, F32), "average": lambda: sync("average"),
+         "recombine": lambda: sync("recombine"), "recombine_mean": lambda: sync("mean"), "split": lambda: sync("split"),
          "adapter_forward_few": lambda: adapters(False, BF16, 5, 72, 88), "adapter_backward_fp32": lambda: adapters(True, F32, 300, 101, 77)}
 
 
@@ -98,7 +143,7 @@ def test_what_a_call_makes_stays_while_its_stream_has_it_to_run(name, scratch):
             torch.cuda._sleep(HOLD)
         out = results_of(call(stream=side))
         made = ranges(out[len(out) - call.made:]) + scratch
-        assert scratch
+        assert scratch or not getattr(call, "scratch", True)
         if not keep:
             out = None
         # as many blocks of every size as the call made, and more, all of them filled
@@ -211,3 +256,24 @@ def test_norms_of_many_calls_are_all_their_own():
     plan = ab.ClipPlan([g], norm_only=True)
     norms = [ab.ab_grad_clip(plan, 1.0)[1] for _ in range(200)]
     assert len({n.data_ptr() for n in norms}) == 200 and len({float(n) for n in norms}) == 1
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_captured_on_a_branch(name):
+    """A call on a stream that joins a capture and leaves it again: what it makes is the graph's."""
+    call = CALLS[name]()
+    want = [t.clone() for t in results_of(call())]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call(stream=side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = results_of(call(stream=side))
+        torch.cuda.current_stream().wait_stream(side)
+    for t in out:
+        t.fill_(3)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(out, want))
