@@ -372,6 +372,15 @@ def _fits(what, t, shape, dtype, dev):
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
 
+def _adapter_ws(ws, x, A, B, dev, stream):
+    """The workspace of an adapter call: the caller's, or one of the call's own."""
+    if ws is None:
+        return _scratch(ab_adapter_workspace_bytes(x, A, B), x.device, stream)
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"ws: expected a contiguous tensor on the current device (cuda:{dev}), got one on {ws.device}, strides {ws.stride()}")
+    return ws
+
+
 def _adapter_ok(x, W, A, B, row_adapter, scale):
     """Checks the inputs of an adapter call; returns (N, n, L, m, r, device).  A and B may be spaced along their first axis."""
     if x.dim() != 2 or A.dim() != 3:
@@ -409,8 +418,7 @@ def ab_adapter_forward(x, W, A, B, row_adapter, scale=None, y=None, T_save=None,
         _fits("T_save", T_save, (N, r), torch.float32, dev)
     elif save_T:
         T_save = _result(x, (N, r), stream, torch.float32)
-    if ws is None:
-        ws = _scratch(ab_adapter_workspace_bytes(x, A, B), x.device, stream)
+    ws = _adapter_ws(ws, x, A, B, dev, stream)
     st = lib().ab_adapter_forward(x.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), _ptr(scale), row_adapter.data_ptr(), y.data_ptr(),
                                   _ptr(T_save), N, m, n, r, L, A.stride(0), B.stride(0), _dt(x), ws.data_ptr(), ws.numel(),
                                   torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
@@ -439,8 +447,7 @@ def ab_adapter_backward(x, dY, W, A, B, row_adapter, scale=None, T_saved=None, w
         _fits("dB", dB, (L, r, n), torch.float32, dev)
     elif "dB" in want:
         dB = _result(x, (L, r, n), stream, torch.float32)
-    if ws is None:
-        ws = _scratch(ab_adapter_workspace_bytes(x, A, B), x.device, stream)
+    ws = _adapter_ws(ws, x, A, B, dev, stream)
     st = lib().ab_adapter_backward(x.data_ptr(), dY.data_ptr(), _ptr(W), A.data_ptr(), B.data_ptr(), _ptr(scale), row_adapter.data_ptr(),
                                    _ptr(T_saved), _ptr(dX), _ptr(dA), _ptr(dB), N, m, n, r, L, A.stride(0), B.stride(0), _dt(x),
                                    ws.data_ptr(), ws.numel(),
