@@ -888,7 +888,7 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
   } else if (warp == 1) {
     if (rank == 0) {
       int slot = 0, ph = 0, it = 0;
-      bool ok = true;
+      bool ok = true, waited = false;
       const uint32_t base = uniform(smem_u32(ring)), idesc = instr_desc_bf16(128 * kCtas, p.bn, p.mn, 0);
       const uint64_t dA = smem_desc_sw128(base, p.mn ? 8192 : 16), dB = smem_desc_sw128(base + kABytes, 16);
       const uint64_t a_step = p.mn ? 128u : 2u, slot_step = (uint64_t)(p.slot_bytes >> 4);
@@ -921,6 +921,9 @@ wide_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUt
           if (++slot == p.ns) { slot = 0; ph ^= 1; }
         }
         if (!ok) break;
+        // What is waited for from here on (the adapters' slabs, accumulators given back) comes only when the kernel in front is done, which may
+        // take longer than a bounded wait may.
+        if (!waited) { dep_wait(); waited = true; }
         ok = for_runs(gid, ngroups, p.rp, [&](int, int g0, int g1, int, int j) {
           if (!mbar_wait_warp(&b->full[slot], ph)) { raise(&b->abort_any, p.status); return false; }
           tc_fence_after();
