@@ -133,15 +133,21 @@ __device__ __forceinline__ void chunk_squares(const ClipTable<kCap>& t, int q, d
   }
 }
 
-// out = g c over chunk q.
+// out = g c over chunk q, c = (float)factor.  A factor below what fp32 holds in full (2^-126; gradients near the type's largest value or a tiny
+// limit) is applied in 64 bits, by one value a thread: rounded to fp32 it would have few bits left, or none.
 template <typename T, int kCap>
-__device__ __forceinline__ void chunk_scaled(const ClipTable<kCap>& t, int q, float c) {
+__device__ __forceinline__ void chunk_scaled(const ClipTable<kCap>& t, int q, double factor) {
   const int i = find_tensor(t, q);
   int64_t from, to;
   chunk_range<T>(t, q, i, from, to);
   const T* g = static_cast<const T*>(t.rec[i].g);
   T* out = static_cast<T*>(t.rec[i].out);
+  const float c = (float)factor;
   if (c == 1.f && g == out) return;                       // nothing to do where it lies
+  if (factor > 0.0 && factor < 1.1754943508222875e-38) {
+    for (int64_t k = from + threadIdx.x; k < to; k += kClipThreads) from_f32(out[k], (float)((double)to_f32(g[k]) * factor));
+    return;
+  }
   if (((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(out)) & 15) != 0) {
     for (int64_t k = from + threadIdx.x; k < to; k += kClipThreads) from_f32(out[k], c == 1.f ? to_f32(g[k]) : to_f32(g[k]) * c);
     return;
@@ -166,9 +172,9 @@ __device__ __forceinline__ void chunk_scaled(const ClipTable<kCap>& t, int q, fl
 }
 
 // The factor; a norm that is infinite or NaN scales nothing: the caller sees it and can drop the step.
-__device__ __forceinline__ float clip_factor(double norm, float max_norm) {
+__device__ __forceinline__ double clip_factor(double norm, float max_norm) {
   const double big = max_norm;
-  return norm > big && norm <= 1.7976931348623157e308 ? (float)(big / norm) : 1.f;
+  return norm > big && norm <= 1.7976931348623157e308 ? big / norm : 1.0;
 }
 
 // part[blockIdx.x]: the sum of the squares of this CTA's chunks (q = blockIdx.x, + grid, ...), on top of what an earlier launch left there
@@ -194,7 +200,7 @@ clip_scale_kernel(const __grid_constant__ ClipTable<kCap> t, int chunks, const d
   const double norm = sqrt(block_sum(acc));
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   if (!write) return;
-  const float c = clip_factor(norm, max_norm);
+  const double c = clip_factor(norm, max_norm);
   for (int b = blockIdx.x; b < chunks; b += gridDim.x) chunk_scaled<T>(t, chunks - 1 - b, c);
 }
 
