@@ -225,7 +225,9 @@ int ab_dense_backward(const void* x, const void* dY, const void* W, void* dX, fl
  *   that are not a's.  An infinity makes its own results infinite or NaN: the general kernels split fp32 values as ab_recombine does.
  *   bf16 with m, n, r, strideA, strideB multiples of 8, r <= 256 and 16-byte aligned pointers runs on the tensor cores (dA and dB where
  *   L * ceil(N / 64) <= 2^24 besides); everything else takes general kernels.  N = 0 is a no-op (dA, dB are zeroed).  N < 2^31.  No output may overlap an input or
- *   another output.  Workspace: ab_adapter_workspace_bytes, for either call.
+ *   another output.  Workspace: ab_adapter_workspace_bytes, for either call: T, U and the rows' order (8 r + 4 bytes a row; on the tensor cores
+ *   T, U, their pieces and lists, at most 20 r + 200 + L / 4), and up to 1 GB of partial products of the general kernels (64 MB where
+ *   the sizes are the tensor cores'), which take the rows in bands where that does not hold all of them.
  */
 int ab_adapter_forward(const void* x, const void* W, const void* A, const void* B, const float* scale, const int* row_adapter,
                        void* y, float* T_save, int64_t N, int m, int n, int r, int L, int64_t strideA, int64_t strideB, int dt,

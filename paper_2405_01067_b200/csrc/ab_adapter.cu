@@ -357,6 +357,23 @@ int base_slices(int64_t N, int P, int K) {
   }
   return best;
 }
+// The slices lie in the workspace for a band of rows at a time, of as many rows as it holds, bands of one length; the bits do not depend on it.  What
+// the query asks for is bounded: up to 1 GB for sizes that always come here, 64 MB beside the tensor-core path, whose sizes come here
+// for misaligned pointers alone.  (8191 rows, 4096 x 4096, rank 16, fp32, forward and backward: 6.3 ms with all 805 MB of slices at once, 6.6 in bands
+// of 256 MB, 6.8 of 128, 7.5 of 64; bf16 4095 x 4097 10.0, 10.7, 11.7, 13.4: a band ends with SMs that have nothing left to do.)
+constexpr int64_t kSliceBytes = (int64_t)1 << 30, kSliceBytesBeside = (int64_t)64 << 20;
+constexpr int64_t kLeastRows = 128;
+// bytes of `rows` rows' slices: none where one slice by itself lies in an fp32 result
+int64_t slice_bytes(int64_t N, int64_t rows, int P, int K, int dt) {
+  const int s = base_slices(N, P, K);
+  return dt == AB_F32 && s == 1 ? 0 : (rows < N ? rows : N) * s * P * (int64_t)sizeof(float);
+}
+int64_t band_rows(int64_t N, int P, int slices, int64_t room) {
+  const int64_t most = room / ((int64_t)slices * P * (int64_t)sizeof(float));
+  if (N <= most) return N;
+  const int64_t whole = most / kLeastRows * kLeastRows, bands = (N + whole - 1) / whole;      // kLeastRows fit (general_ws)
+  return ((N + bands - 1) / bands + kLeastRows - 1) / kLeastRows * kLeastRows;
+}
 // Small products stay on the fp32 pipes (128 x 512 x 256: 11.6 us against 12.0, and no slices)
 bool base_small(const Call& c, int P, int K) { return c.dt == AB_F32 && gemm_small_pays(c.N, P, K); }
 
@@ -369,26 +386,34 @@ int grad_slices(int64_t N, int m, int n, int r, int L) {
   return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
 }
 
-// Workspace of the general path: status word, T, U, the shared product, the adapters' rows, the gradients' slices
-struct GeneralWs { int* status; float *T, *U, *base; int* order; int64_t *start, *count; float *pA, *pB; int slices; size_t bytes; };
-GeneralWs general_ws(void* ws, int64_t N, int m, int n, int r, int L, int dt) {
+// Workspace of the general path: status word, T, U, the adapters' rows, the gradients' slices, and in what is left (room, bytes) a band of the
+// shared product.  bytes: the least that it runs with.
+struct GeneralWs { int* status; float *T, *U, *base; int* order; int64_t *start, *count; float *pA, *pB; int slices; int64_t room; size_t bytes; };
+GeneralWs general_ws(void* ws, size_t ws_bytes, int64_t N, int m, int n, int r, int L, int dt) {
   Arena ar(ws, 0);
   GeneralWs w;
   w.status = ar.take_n<int>(64);
   w.T = ar.take_n<float>((size_t)N * r);
   w.U = ar.take_n<float>((size_t)N * r);
-  const int sy = base_slices(N, m, n), sx = base_slices(N, n, m);
-  const size_t y = (size_t)sy * m, x = (size_t)sx * n;
-  const bool none = dt == AB_F32 && sy == 1 && sx == 1;      // a slice by itself lies in an fp32 result
-  w.base = none ? nullptr : ar.take_n<float>((size_t)N * (x > y ? x : y));
   w.order = ar.take_n<int>((size_t)N);
   w.start = ar.take_n<int64_t>((size_t)L);
   w.count = ar.take_n<int64_t>((size_t)L);
   w.slices = grad_slices(N, m, n, r, L);
   w.pA = w.slices > 1 ? ar.take_n<float>((size_t)w.slices * L * m * r) : nullptr;
   w.pB = w.slices > 1 ? ar.take_n<float>((size_t)w.slices * L * n * r) : nullptr;
-  w.bytes = align_up(ar.used, 256);
+  w.base = ar.take_n<float>(0);
+  w.room = ws_bytes > ar.used ? (int64_t)(ws_bytes - ar.used) : 0;
+  const int64_t y = slice_bytes(N, kLeastRows, m, n, dt), x = slice_bytes(N, kLeastRows, n, m, dt);
+  w.bytes = align_up(ar.used + (size_t)(x > y ? x : y), 256);
   return w;
+}
+// What the query asks for: the slices of all rows, up to `most` bytes
+size_t general_ws_bytes(int64_t N, int m, int n, int r, int L, int dt, int64_t most) {
+  const size_t least = general_ws(nullptr, 0, N, m, n, r, L, dt).bytes;
+  const int64_t y = slice_bytes(N, N, m, n, dt), x = slice_bytes(N, N, n, m, dt), all = x > y ? x : y;
+  const int64_t y0 = slice_bytes(N, kLeastRows, m, n, dt), x0 = slice_bytes(N, kLeastRows, n, m, dt), some = x0 > y0 ? x0 : y0;
+  const int64_t more = (all < most ? all : most) - some;
+  return align_up(least + (size_t)(more > 0 ? more : 0), 256);
 }
 
 template <typename TI, int kRB>
@@ -405,47 +430,56 @@ int project(const Call& c, const void* In, int K, const void* F, int64_t strideF
               : launch_project<bf16, 1>(c, In, K, F, strideF, f_k, f_j, T, first, status);
 }
 
+// rows [row0, row0 + rows) of the call; base: their slices
 template <typename T16, int kRD>
-int launch_delta(const Call& c, const float* base, int slices, const float* T, const void* G, int64_t strideG, int64_t g_c, int64_t g_k, void* out,
-                 int P, int* status) {
-  const dim3 grid((unsigned)((c.N + kRD - 1) / kRD), (unsigned)((P + kDeltaCols - 1) / kDeltaCols));
-  return launch_after(delta_kernel<T16, T16, kRD>, grid, (unsigned)kDeltaCols, 0, 1, c.st, base, slices, T, static_cast<const T16*>(G), strideG, g_c,
-                      g_k, c.ids, static_cast<T16*>(out), c.N, P, c.r, c.L, status);
+int launch_delta(const Call& c, int64_t row0, int64_t rows, const float* base, int slices, const float* T, const void* G, int64_t strideG, int64_t g_c,
+                 int64_t g_k, void* out, int P, int* status) {
+  const dim3 grid((unsigned)((rows + kRD - 1) / kRD), (unsigned)((P + kDeltaCols - 1) / kDeltaCols));
+  return launch_after(delta_kernel<T16, T16, kRD>, grid, (unsigned)kDeltaCols, 0, 1, c.st, base, slices, T + row0 * c.r, static_cast<const T16*>(G),
+                      strideG, g_c, g_k, c.ids + row0, static_cast<T16*>(out) + row0 * P, rows, P, c.r, c.L, status);
+}
+template <typename T16>
+int delta(const Call& c, int64_t row0, int64_t rows, const float* base, int slices, const float* T, const void* G, int64_t strideG, int64_t g_c,
+          int64_t g_k, void* out, int P, int* status) {
+  // sixteen rows a block where that still gives every SM two blocks
+  const int sms = sm_count() > 0 ? sm_count() : 148;
+  const int64_t blocks = (rows + 15) / 16 * ((P + kDeltaCols - 1) / kDeltaCols);
+  return blocks >= 2 * sms ? launch_delta<T16, 16>(c, row0, rows, base, slices, T, G, strideG, g_c, g_k, out, P, status)
+                           : launch_delta<T16, 2>(c, row0, rows, base, slices, T, G, strideG, g_c, g_k, out, P, status);
 }
 
 // out = In W^T (W: P x K, row-major) or In W (W: K x P), and T's part
 int shared_and_delta(const Call& c, const void* In, int K, bool w_mn, const float* T, const void* G, int64_t strideG, int64_t g_c, int64_t g_k,
                      void* out, int P, const GeneralWs& w) {
-  const int sms = sm_count() > 0 ? sm_count() : 148;
-  float* base = w.base;
-  int slices = 1;
-  if (base_small(c, P, K) || !gemm_tc_available() || c.N > 0x3fffffff) {
-    if (c.dt == AB_F32) base = static_cast<float*>(out);
-    AB_TRY(gemm_simt(In, c.dt, K, 1, c.W, c.dt, w_mn ? P : 1, w_mn ? 1 : K, base, AB_F32, P, c.N, P, K, c.st));
-  } else {
-    slices = base_slices(c.N, P, K);
-    if (c.dt == AB_F32 && slices == 1) base = static_cast<float*>(out);
-    const int per = ((K + slices - 1) / slices + 63) / 64 * 64;
-    const int64_t e = (int64_t)dtype_size(c.dt);
-    SplitGemm p[kSplitFew];
-    memset(p, 0, sizeof(p));
-    int n = 0;
-    for (int k0 = 0; k0 < K; k0 += per, ++n) {
-      p[n].A = static_cast<const char*>(In) + k0 * e; p[n].lda = K;
-      p[n].B = static_cast<const char*>(c.W) + (w_mn ? (int64_t)k0 * P : (int64_t)k0) * e; p[n].ldb = w_mn ? P : K; p[n].b_mn = w_mn ? 1 : 0;
-      p[n].C = base + (int64_t)n * c.N * P; p[n].ldc = P;
-      p[n].M = (int)c.N; p[n].N = P; p[n].K = K - k0 < per ? K - k0 : per;
+  const bool simt = base_small(c, P, K) || !gemm_tc_available() || c.N > 0x3fffffff;
+  const int want = base_slices(c.N, P, K);
+  const bool in_place = c.dt == AB_F32 && (simt || want == 1);       // the product lies in the result
+  const int64_t e = (int64_t)dtype_size(c.dt), band = in_place ? c.N : band_rows(c.N, P, want, w.room);
+  for (int64_t row0 = 0; row0 < c.N; row0 += band) {
+    const int64_t rows = c.N - row0 < band ? c.N - row0 : band;
+    const char* X = static_cast<const char*>(In) + row0 * K * e;
+    float* base = in_place ? static_cast<float*>(out) : w.base;
+    int slices = 1;
+    if (simt) {
+      AB_TRY(gemm_simt(X, c.dt, K, 1, c.W, c.dt, w_mn ? P : 1, w_mn ? 1 : K, base, AB_F32, P, rows, P, K, c.st));
+    } else {
+      const int per = ((K + want - 1) / want + 63) / 64 * 64;
+      SplitGemm p[kSplitFew];
+      memset(p, 0, sizeof(p));
+      int n = 0;
+      for (int k0 = 0; k0 < K; k0 += per, ++n) {
+        p[n].A = X + k0 * e; p[n].lda = K;
+        p[n].B = static_cast<const char*>(c.W) + (w_mn ? (int64_t)k0 * P : (int64_t)k0) * e; p[n].ldb = w_mn ? P : K; p[n].b_mn = w_mn ? 1 : 0;
+        p[n].C = base + (int64_t)n * rows * P; p[n].ldc = P;
+        p[n].M = (int)rows; p[n].N = P; p[n].K = K - k0 < per ? K - k0 : per;
+      }
+      slices = n;
+      AB_TRY(gemm_split_few(p, n, c.dt == AB_BF16, w.status, c.st));
     }
-    slices = n;
-    AB_TRY(gemm_split_few(p, n, c.dt == AB_BF16, w.status, c.st));
+    AB_TRY(c.dt == AB_F32 ? delta<float>(c, row0, rows, base, slices, T, G, strideG, g_c, g_k, out, P, w.status)
+                          : delta<bf16>(c, row0, rows, base, slices, T, G, strideG, g_c, g_k, out, P, w.status));
   }
-  // sixteen rows a block where that still gives every SM two blocks
-  const int64_t blocks = (c.N + 15) / 16 * ((P + kDeltaCols - 1) / kDeltaCols);
-  if (c.dt == AB_F32)
-    return blocks >= 2 * sms ? launch_delta<float, 16>(c, base, slices, T, G, strideG, g_c, g_k, out, P, w.status)
-                             : launch_delta<float, 2>(c, base, slices, T, G, strideG, g_c, g_k, out, P, w.status);
-  return blocks >= 2 * sms ? launch_delta<bf16, 16>(c, base, slices, T, G, strideG, g_c, g_k, out, P, w.status)
-                           : launch_delta<bf16, 2>(c, base, slices, T, G, strideG, g_c, g_k, out, P, w.status);
+  return AB_OK;
 }
 
 int grads(const Call& c, const GeneralWs& w, const void* dY, const float* T, float* dA, float* dB) {
@@ -513,8 +547,8 @@ extern "C" {
 
 size_t ab_adapter_workspace_bytes(int64_t N, int m, int n, int r, int L, int dt) {
   if (N < 0 || N > 0x7fffffffll || m <= 0 || n <= 0 || r <= 0 || L <= 0 || !dtype_ok(dt)) return 0;
-  const size_t g = general_ws(nullptr, N, m, n, r, L, dt).bytes;
-  const size_t t = adapter_tc_shape_ok(N, m, n, r, L, dt) ? adapter_tc_ws(N, m, n, r, L) : 0;
+  const bool tc = adapter_tc_shape_ok(N, m, n, r, L, dt);
+  const size_t g = general_ws_bytes(N, m, n, r, L, dt, tc ? kSliceBytesBeside : kSliceBytes), t = tc ? adapter_tc_ws(N, m, n, r, L) : 0;
   return (g > t ? g : t) + 256;
 }
 
@@ -531,7 +565,7 @@ int ab_adapter_forward(const void* x, const void* W, const void* A, const void* 
     if (adapter_tc_ws(N, m, n, r, L) > ws_bytes) return AB_ERR_WORKSPACE;
     return adapter_tc_forward(c, y, T_save, ws);
   }
-  const GeneralWs w = general_ws(ws, N, m, n, r, L, dt);
+  const GeneralWs w = general_ws(ws, ws_bytes, N, m, n, r, L, dt);
   if (w.bytes > ws_bytes) return AB_ERR_WORKSPACE;
   return general_forward(c, y, T_save, w);
 }
@@ -560,7 +594,7 @@ int ab_adapter_backward(const void* x, const void* dY, const void* W, const void
     if (adapter_tc_ws(N, m, n, r, L) > ws_bytes) return AB_ERR_WORKSPACE;
     return adapter_tc_backward(c, dY, T_saved, dX, dA, dB, ws);
   }
-  const GeneralWs w = general_ws(ws, N, m, n, r, L, dt);
+  const GeneralWs w = general_ws(ws, ws_bytes, N, m, n, r, L, dt);
   if (w.bytes > ws_bytes) return AB_ERR_WORKSPACE;
   return general_backward(c, dY, T_saved, dX, dA, dB, w);
 }

@@ -84,3 +84,13 @@ def test_clip_refusals(b):
 def test_workspace_of_many_adapters_stays_small(b):
     """The lists behind the gradients are bounded whatever the number of adapters: 2^20 adapters beside 2^20 rows."""
     assert 0 < b.lib().ab_adapter_workspace_bytes(1 << 20, 64, 64, 8, 1 << 20, b.AB_BF16) < 1 << 31
+
+
+@pytest.mark.parametrize("N,m,n", [(8191, 4096, 4096), (65536, 4096, 4096), (262144, 4096, 4096), (32768, 8192, 28672), (1 << 20, 4096, 4096)])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_workspace_of_many_rows_stays_small(b, N, m, n, bf16):
+    """Beside T, U, their pieces and what the rows' lists take (under 2 KB a row here) there is a bounded part: 64 MB for sizes of the
+    tensor-core path, 1 GB for the others.  The results' fp32 slices are not all there at a time."""
+    need = b.lib().ab_adapter_workspace_bytes(N, m, n, 16, 8, b.AB_BF16 if bf16 else b.AB_F32)
+    assert 0 < need <= 2048 * N + ((64 << 20) if bf16 else (1 << 30)) + 1024
+    assert b.lib().ab_adapter_workspace_bytes(N, m + 1, n, 15, 8, b.AB_BF16) <= 2048 * N + (1 << 30) + 1024
