@@ -236,6 +236,11 @@ int ab_adapter_backward(const void* x, const void* dY, const void* W, const void
                         const int* row_adapter, const float* T_saved, void* dX, float* dA, float* dB, int64_t N, int m, int n, int r,
                         int L, int64_t strideA, int64_t strideB, int dt, void* ws, size_t ws_bytes, void* cuda_stream);
 size_t ab_adapter_workspace_bytes(int64_t N, int m, int n, int r, int L, int dt);
+/*
+ * For tests: the form in which the tensor-core path makes an N x P result of a reduction of K (forward: P = m, K = n; dX: P = n, K = m) on
+ * the current device (148 SMs where there is none).  0: few rows; else the rows of a tile, + 1 where CTAs have tiles in pairs; -1: no sizes.
+ */
+int ab_selftest_adapter_form(int64_t N, int P, int K);
 
 /*
  * One AdamW update of a factor from the gradient ab_layer_backward left (the paper trains with

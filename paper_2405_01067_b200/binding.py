@@ -29,7 +29,7 @@ EXPORTS = ["ab_status_string", "ab_version", "ab_launch_count", "ab_workspace_by
            "ab_selftest_split_fallback", "ab_selftest_split_fallback_workspace_bytes",
            "ab_dense_forward", "ab_dense_backward", "ab_conv3x3_forward", "ab_conv3x3_backward",
            "ab_conv3x3_workspace_bytes", "ab_recombine_mean", "ab_adapter_forward", "ab_adapter_backward",
-           "ab_adapter_workspace_bytes", "ab_grad_clip", "ab_grad_clip_workspace_bytes"]
+           "ab_adapter_workspace_bytes", "ab_selftest_adapter_form", "ab_grad_clip", "ab_grad_clip_workspace_bytes"]
 
 
 class AbError(RuntimeError):
@@ -74,6 +74,8 @@ def lib() -> ctypes.CDLL:
     L.ab_adapter_forward.argtypes = [c_void_p] * 8 + [c_int64] + [c_int] * 4 + [c_int64] * 2 + [c_int, c_void_p, c_size_t, c_void_p]
     L.ab_adapter_backward.restype = c_int
     L.ab_adapter_backward.argtypes = [c_void_p] * 11 + [c_int64] + [c_int] * 4 + [c_int64] * 2 + [c_int, c_void_p, c_size_t, c_void_p]
+    L.ab_selftest_adapter_form.restype = c_int
+    L.ab_selftest_adapter_form.argtypes = [c_int64, c_int, c_int]
     L.ab_adapter_workspace_bytes.restype = c_size_t
     L.ab_adapter_workspace_bytes.argtypes = [c_int64] + [c_int] * 5
     L.ab_group_average.restype = c_int

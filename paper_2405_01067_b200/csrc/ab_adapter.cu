@@ -552,6 +552,8 @@ size_t ab_adapter_workspace_bytes(int64_t N, int m, int n, int r, int L, int dt)
   return (g > t ? g : t) + 256;
 }
 
+int ab_selftest_adapter_form(int64_t N, int P, int K) { return N < 1 || P < 1 || K < 1 ? -1 : adapter_tc_form(N, P, K); }
+
 int ab_adapter_forward(const void* x, const void* W, const void* A, const void* B, const float* scale, const int* row_adapter,
                        void* y, float* T_save, int64_t N, int m, int n, int r, int L, int64_t strideA, int64_t strideB, int dt,
                        void* ws, size_t ws_bytes, void* cuda_stream) {

@@ -1573,6 +1573,23 @@ int launch_project(const AdapterCall& c, const void* In, int K, const void* F, i
   return launch_after(project_tc_kernel<8>, grid, (unsigned)kProjTcThreads, smem, p.csize, c.st, tmIn, tmF, p);
 }
 
+// CTAs by themselves or in pairs, and the rows of a tile: cycles of the busiest SM, a slab's operands arriving at 64 bytes a cycle or its
+// MMAs, whichever is longer
+struct WideForm { int bn; bool pair; };
+WideForm wide_form(int64_t N, int P, int K, int sms) {
+  const int nk = (K + 63) / 64;
+  double best = 1e30;
+  WideForm f = {256, false};
+  for (int two = 0; two < 2; ++two)
+    for (int bn = 32 << two; bn <= 256; bn *= 2) {
+      const int64_t tiles = (int64_t)((P + (128 << two) - 1) / (128 << two)) * ((N + bn - 1) / bn);
+      const double mma = bn <= 64 ? 300.0 : bn <= 128 ? 330.0 : 560.0, arrive = 2.0 * (128 + (bn >> two));
+      const double t = (double)((tiles + (sms >> two) - 1) / (sms >> two)) * (nk + 2) * (arrive > mma ? arrive : mma) + (two ? 4500.0 : 3000.0);
+      if (t < best) { best = t; f.bn = bn; f.pair = two != 0; }
+    }
+  return f;
+}
+
 // Out = In W^T + T G^T; mn as in OutParams
 int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void* G, int64_t strideG, void* Out, int P, const float* T, const bf16* Tp,
                int* status) {
@@ -1613,17 +1630,9 @@ int launch_out(const AdapterCall& c, const void* In, int K, bool mn, const void*
     return launch_after(few_kernel, dim3((unsigned)(p.nft * p.csize), (unsigned)tt), (unsigned)kWideThreads,
                         1024 + (size_t)p.ns * p.slot_bytes + rest, p.csize, c.st, tmW, tmIn, p);
   }
-  // CTAs by themselves or in pairs, and the rows of a tile: cycles of the busiest SM, a slab's operands arriving at 64 bytes a cycle or its
-  // MMAs, whichever is longer
-  double best = 1e30;
-  bool pair = false;
-  for (int two = 0; two < 2; ++two)
-    for (int bn = 32 << two; bn <= 256; bn *= 2) {
-      const int64_t tiles = (int64_t)((P + (128 << two) - 1) / (128 << two)) * ((c.N + bn - 1) / bn);
-      const double mma = bn <= 64 ? 300.0 : bn <= 128 ? 330.0 : 560.0, arrive = 2.0 * (128 + (bn >> two));
-      const double t = (double)((tiles + (sms >> two) - 1) / (sms >> two)) * (p.nk + 2) * (arrive > mma ? arrive : mma) + (two ? 4500.0 : 3000.0);
-      if (t < best) { best = t; p.bn = bn; pair = two != 0; }
-    }
+  const WideForm f = wide_form(c.N, P, K, sms);
+  const bool pair = f.pair;
+  p.bn = f.bn;
   const int ctas = pair ? 2 : 1;
   p.nft = (P + 128 * ctas - 1) / (128 * ctas);
   const int64_t tiles = (int64_t)p.nft * ((c.N + p.bn - 1) / p.bn);
@@ -1738,6 +1747,13 @@ bool adapter_tc_supported(const AdapterCall& c, const void* dY, const void* out,
   if (c.L > 1 && (c.strideA % 8 != 0 || c.strideB % 8 != 0)) return false;
   return aligned(c.x, 16) && aligned(c.W, 16) && aligned(c.A, 16) && aligned(c.B, 16) && aligned(dY, 16) && aligned(out, 16) && aligned(T, 16) &&
          aligned(dA, 16) && aligned(dB, 16) && tc_device_ok();
+}
+
+// For tests: which kernel forms N x P results over a reduction of K. 0: the one for few rows; else the rows of a tile, + 1 where CTAs go in pairs.
+int adapter_tc_form(int64_t N, int P, int K) {
+  if (few_rows(N, P)) return 0;
+  const WideForm f = wide_form(N, P, K, sm_count() > 0 ? sm_count() : 148);
+  return f.bn + (f.pair ? 1 : 0);
 }
 
 size_t adapter_tc_ws(int64_t N, int m, int n, int r, int L) { return tc_ws(nullptr, N, m, n, r, L).bytes; }
