@@ -220,9 +220,14 @@ int ab_dense_backward(const void* x, const void* dY, const void* W, void* dX, fl
  *   T_save: NULL, or fp32 [N,r] that receives T (0 in rows without an adapter) for the backward call; T_saved NULL recomputes it from x.
  *   dA [L,m,r], dB [L,r,n]: fp32, dense, every element written: 0 for an adapter without rows.  W is not trained here (ab_dense_backward
  *   has dW).  Any of dX, dA, dB may be NULL; W may be NULL where dX is.
- *   Sums are held in fp32 or more and y, dX rounded once.  Sums run in a fixed order: two runs give identical bits.  No row's result
- *   depends on another row, nor on an adapter that is not its own, also where those hold infinities or NaN; nor does dA_a or dB_a on rows
- *   that are not a's.  An infinity makes its own results infinite or NaN: the general kernels split fp32 values as ab_recombine does.
+ *   Sums are held in fp32 or more and y, dX rounded once.  The tensor cores cut a sum off at every sixteenth term instead of rounding it (2^-23 of
+ *   it at most, measured 2e-8): in bf16 that goes over the whole reduction of W x and W^T dY (5e-6 of it over 4096 terms, one-sided, where a
+ *   result's rounding is up to 4e-3), and over 256 terms at a time in T, U, dA and dB.  T and U have all 24 bits in the gradients; the second
+ *   product of many rows in bf16 takes 16 of them (2^-16 of A_a T_i at most).  Where W x_i and A_a T_i nearly cancel, both show.
+ *   Sums run in a fixed order: two runs give identical bits.  No row's result depends on what another row holds, nor on an adapter that is
+ *   not its own, also where those are infinities or NaN; nor does dA_a or dB_a on rows that are not a's.  (The way a row's sums are formed, and with
+ *   it the last bits of its result, goes by the sizes and by which adapters the rows beside it have.)  An infinity makes its own
+ *   results infinite or NaN: the general kernels split fp32 values as ab_recombine does.
  *   bf16 with m, n, r, strideA, strideB multiples of 8, r <= 256 and 16-byte aligned pointers runs on the tensor cores (dA and dB where
  *   L * ceil(N / 64) <= 2^24 besides); everything else takes general kernels.  N = 0 is a no-op (dA, dB are zeroed).  N < 2^31.  No output may overlap an input or
  *   another output.  Workspace: ab_adapter_workspace_bytes, for either call: T, U and the rows' order (8 r + 4 bytes a row; on the tensor cores

@@ -14,12 +14,12 @@
 //   few_kernel      the same for few rows (generation): bound by the reading of W, whose reduction is cut over a cluster
 //   adapter_grad    D_a = In^T T over the 64-row slabs that have rows of a; rows of others in such a slab are cleared in shared memory
 //
-// Measured, us (floor: the bytes or operations a call cannot do without, at 6538 GB/s and 1679 TFLOP/s): one token, 4096 x 4096, rank 16 16
-// (5.2); 64 tokens of 64 adapters 17 (7.9); 6173 rows of 16 adapters, 2048 -> 8192, rank 64 214 (128; wide_kernel 1180 TFLOP/s);
-// training, 50,432 rows of 4 groups, 768 x 768, rank 64 237 (89); 8191 rows of 8, 4096 x 4096, rank 16 505 (331).
+// Measured, us (floor: the bytes or operations a call cannot do without, at 6538 GB/s and 1679 TFLOP/s): one token, 4096 x 4096, rank 16 15, of
+// which 10 are the kernels' (5.2); 64 tokens of 64 adapters 17 (7.9); 6173 rows of 16 adapters, 2048 -> 8192, rank 64 214 (128); training, 50,432
+// rows of 4 groups, 768 x 768, rank 64 240 (89); 8191 rows of 8, 4096 x 4096, rank 16 515 (331).
 //
 // T travels as three bf16 pieces (hi = bf16(T), mid = bf16(T - hi), lo the rest: 24 bits): the second product takes two of them (its result
-// is rounded to bf16, 2^-17 of T is lost), the gradients take all three.
+// is rounded to bf16, of whose half step, 2^-8, the 2^-16 of T that is lost at most is nothing), the gradients take all three.
 #include <cstring>
 
 #include "ab_adapter.cuh"
