@@ -366,7 +366,8 @@ constexpr int64_t kLeastRows = 128;
 // bytes of `rows` rows' slices: none where one slice by itself lies in an fp32 result
 int64_t slice_bytes(int64_t N, int64_t rows, int P, int K, int dt) {
   const int s = base_slices(N, P, K);
-  return dt == AB_F32 && s == 1 ? 0 : (rows < N ? rows : N) * s * P * (int64_t)sizeof(float);
+  const int64_t row = (int64_t)s * P * (int64_t)sizeof(float), n = rows < N ? rows : N;
+  return dt == AB_F32 && s == 1 ? 0 : n > INT64_MAX / row ? INT64_MAX : n * row;
 }
 int64_t band_rows(int64_t N, int P, int slices, int64_t room) {
   const int64_t most = room / ((int64_t)slices * P * (int64_t)sizeof(float));

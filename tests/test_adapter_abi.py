@@ -94,3 +94,12 @@ def test_workspace_of_many_rows_stays_small(b, N, m, n, bf16):
     need = b.lib().ab_adapter_workspace_bytes(N, m, n, 16, 8, b.AB_BF16 if bf16 else b.AB_F32)
     assert 0 < need <= 2048 * N + ((64 << 20) if bf16 else (1 << 30)) + 1024
     assert b.lib().ab_adapter_workspace_bytes(N, m + 1, n, 15, 8, b.AB_BF16) <= 2048 * N + (1 << 30) + 1024
+
+
+def test_workspace_of_sizes_whose_slices_pass_64_bits(b):
+    """2^31 - 1 rows of 2^31 - 1 values in eight slices are more than 2^63 bytes: the bounded part stays what it is."""
+    most = (1 << 31) - 1
+    rows = b.lib().ab_adapter_workspace_bytes(most, 64, 64, 1, 1, b.AB_F32)
+    assert rows >= 12 * most
+    for dt in (b.AB_F32, b.AB_BF16):
+        assert rows <= b.lib().ab_adapter_workspace_bytes(most, most, 10_000, 1, 1, dt) <= rows + 128 * 8 * 4 * most + (2 << 30)
