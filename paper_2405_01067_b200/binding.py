@@ -476,7 +476,7 @@ def ab_adamw_step(param, grad, m, v, lr, step, beta1=0.9, beta2=0.999, eps=1e-8,
 
 class ClipPlan:
     """Descriptors of the clipping of one step's gradients (ab_grad_clip): tensors of one type at addresses that stay, as an optimizer's do.
-    Gradients that are made anew every step (set to None behind it) want a plan a step: a plan kept over them scales the old ones.  out:
+    Gradients that are made anew every step (set to None behind it) go to ab_grad_clip themselves: a plan kept over them scales the old ones.  out:
     tensors that receive the scaled values (None: in place); norm_only leaves the gradients alone.  norm: what the last call returned."""
 
     def __init__(self, grads, out=None, norm_only=False):
@@ -509,10 +509,12 @@ class ClipPlan:
         self.norms = list(torch.empty(64, dtype=torch.float32, device=self.grads[0].device).unbind())
 
 
-def ab_grad_clip(plan: ClipPlan, max_norm: float, stream=None):
-    """Scales the plan's gradients by max_norm / norm where their global norm is above max_norm.  Returns (outputs or None, norm), norm a
-    device tensor of one fp32 value, of this call alone; one that is not finite scales nothing.  The plan may go when the call returns; its
-    tensors stay until the stream has run it."""
+def ab_grad_clip(plan, max_norm: float, stream=None):
+    """Scales the gradients of a ClipPlan, or those of a list in place, by max_norm / norm where their global norm is above max_norm.  Returns
+    (outputs or None, norm), norm a device tensor of one fp32 value, of this call alone; one that is not finite scales nothing.  The plan
+    may go when the call returns; its tensors stay until the stream has run it."""
+    if not isinstance(plan, ClipPlan):
+        plan = ClipPlan(plan)
     dev = torch._C._cuda_getDevice()
     if plan.dev != dev:
         raise ValueError("the plan's tensors must be on the current device")

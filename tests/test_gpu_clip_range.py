@@ -33,3 +33,19 @@ def test_factors_below_fp32(count, value, max_norm, shift, dtype):
         got = out.float().cpu().numpy().astype(np.float64)
         step, least = (2.0 ** -24, 2.0 ** -150) if dtype == F32 else (2.0 ** -8 + 2.0 ** -23, 2.0 ** -134 + 2.0 ** -149)
         assert (np.abs(got - want) <= step * np.abs(want) * (1 + 2.0 ** -20) + least * (1 + 2.0 ** -20)).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_list_of_gradients(dtype):
+    """Without a plan: other tensors every step, as a backward pass leaves them that found none."""
+    for step in range(3):
+        g = torch.Generator(device="cuda").manual_seed(step)
+        grads = [torch.randn(k, device="cuda", generator=g).to(dtype) for k in (1000, 77, 5)]
+        copies = [t.clone() for t in grads]
+        out, norm = ab.ab_grad_clip(grads if step else iter(grads), 1.0)
+        want, norm2 = ab.ab_grad_clip(ab.ClipPlan(copies), 1.0)
+        assert torch.equal(norm, norm2) and len(out) == 3
+        assert all(p is q and torch.equal(p, w) for p, q, w in zip(out, grads, want))
+    for bad in ([], [torch.ones(3)], [torch.ones(3, device="cuda"), torch.ones(3, device="cuda", dtype=torch.float64)]):
+        with pytest.raises((ValueError, TypeError)):
+            ab.ab_grad_clip(bad, 1.0)
