@@ -1,5 +1,5 @@
 """The general path of the adapters with a workspace that holds the shared product's slices of some rows alone: several bands of rows, the last
-one shorter, with the bits of one band, whose results test_gpu_adapter.check holds against the checker."""
+one shorter, with the bits of one band, whose results test_gpu_adapter.check holds against the oracle."""
 import pytest
 import torch
 
